@@ -270,6 +270,87 @@ HB_API int hb_eco_scan(const int64_t *share0, const int64_t *share1, size_t n, u
  */
 HB_API int hb_eco_choose(const uint64_t *counts);
 
+/*
+ * What stands before and after a ReLU in a decoder layer on shares: a linear layer with public 4-bit weights, a paged cache of keys and values,
+ * and attention over it.  Every product of two numbers at 2^16 fixed point is followed by a truncation on shares (Sec. 2.2: products are rescaled).
+ *
+ * Truncation of y = y_0 + y_1, -2^62 <= y < 2^62 (read as signed), by f bits, with four dealer words v_0 .. v_3: r = v_0 + v_1;
+ * c = (y_0 + v_0) + (y_1 + v_1) + 2^62 is opened (64 bits); with c_m = c >> 63, g = 2^(63-f) (1 - 2 c_m):
+ *   t_0 = ((c mod 2^63) >> f) + c_m 2^(63-f) - 2^(62-f) - v_2 + g v_3,
+ *   t_1 = g ((r >> 63) - v_3) - (((r mod 2^63) >> f) - v_2).
+ * t_0 + t_1 is floor(y / 2^f), or one more where the lower f bits of y and r carry.  Outside the stated range the result is unspecified.
+ */
+#define HB_LINEAR_MAX ((size_t)1 << 24)   /* most rows, inputs, outputs and tokens of one call */
+#define HB_CACHE_MAX_DIM 256
+
+/*
+ * Linear layer on shares with public 4-bit weights and group scales (no messages but those of the truncation):
+ *   y_p[r][n] = sum over j < in of S[n][j / group] q[n][j] x_p[r][j]  (mod 2^64),  out = truncation of y by `frac` bits.
+ * weight: DEVICE, out x ceil(in / 2) bytes; byte j of a row holds inputs 2j (lower four bits) and 2j + 1, as numbers in -8 .. 7 in two's
+ * complement; the upper half of a last byte that no input has is not used.  scales: DEVICE, out x ceil(in / group) int32 S = round(2^frac s),
+ * 4-byte aligned.  group: a positive multiple of 32; frac: 1 .. 31.  x0, x1: rows x in; out0, out1: rows x out; 8-byte aligned, the outputs
+ * overlapping nothing.  in >= 1; rows == 0 or out == 0 is a successful no-op.
+ * Dealer words of output i = r * out + n: A[4i .. 4i+3], A the arithmetic stream of `seed` (the one of hb_relu: give every call its own seed).
+ * opened_bits receives 64 rows out.
+ */
+HB_API int hb_linear_q4(const int64_t *x0, const int64_t *x1, size_t rows, size_t in, size_t out, const uint8_t *weight, const int32_t *scales,
+                        int group, int frac, uint64_t seed, int64_t *out0, int64_t *out1, uint64_t *opened_bits, void *stream);
+
+/*
+ * A paged cache of keys and values.  It holds masked numbers: x - b for a key or value x, which both parties learn when x is appended; b = b_0 + b_1
+ * stays secret, so that one int64 in memory serves both parties and a product with the cache opens nothing of it again (Beaver's product with a
+ * mask that stays).  The masks of number e = (head * page + offset) * dim + d of a page are words 2e (party 0) and 2e + 1 (party 1) of a stream
+ * started at output 0 (keys) or 1 (values) of the stream started at the page's seed.  A page's seed travels with its contents; a page that
+ * is given to other tokens gets a new one, and a slot is written once under a seed: two numbers under one mask show their difference.
+ * keys, values: DEVICE, pages x heads x page x dim int64.  page_seeds: DEVICE, one uint64 per page.  page: tokens per page, 1 .. 65536; heads:
+ * 1 .. 4096; dim: even, up to HB_CACHE_MAX_DIM.  The struct is read before a call returns.
+ */
+typedef struct hb_cache {
+    int64_t *keys, *values;
+    const uint64_t *page_seeds;
+    size_t pages;
+    int heads, page, dim;
+} hb_cache;
+
+/*
+ * Appends `tokens` keys and values (k0 .. v1: tokens x heads x dim shares) at slots[t] = page * (tokens per page) + offset, and rotates keys and
+ * queries by their positions on the way.  With c, s = row positions[t] of cos and sin (DEVICE int32, table_rows x rot/2, at 2^frac), h = rot/2:
+ *   x'[d] = truncation by frac of x[d] c[d] - x[d+h] s[d],  x'[d+h] = truncation of x[d+h] c[d] + x[d] s[d]   (d < h);
+ * dimensions from rot on are kept.  Queries (q0, q1: tokens x q_heads x dim; q_heads 0: none, pointers unused) go to q_out0, q_out1, with
+ * c and s replaced by (c q_mul + 2^(frac-1)) >> frac, and likewise of s; dimensions from rot on become the truncation of x q_mul: q_mul = 2^frac /
+ * sqrt(dim) is attention's usual factor.  q_out may be the very same buffers as q; what is written overlaps nothing else.
+ * A row whose slot or (rot > 0) position is out of range is padding: nothing of it is written.  Slots of one call are distinct.
+ * rot: even, 0 .. dim (0: positions, cos and sin are unused); frac: 1 .. 30.
+ * Dealer words: A[4i .. 4i+3] of `seed` for number i, the keys (t * heads + head) * dim + d first, then the queries.
+ * opened_bits receives 64 tokens (heads (rot + 2 dim) + q_heads dim).
+ */
+HB_API int hb_cache_append(const hb_cache *cache, const int64_t *k0, const int64_t *k1, const int64_t *v0, const int64_t *v1, size_t tokens,
+                           const int64_t *slots, const int32_t *positions, const int32_t *cos, const int32_t *sin, size_t table_rows, int rot,
+                           int frac, const int64_t *q0, const int64_t *q1, int q_heads, int32_t q_mul, uint64_t seed, int64_t *q_out0,
+                           int64_t *q_out1, uint64_t *opened_bits, void *stream);
+
+/*
+ * Attention of one new token per sequence over the cache, with ReLU(score) / length as the weights (softmax has no short circuit on shares):
+ *   s[t] = truncation by 16 of sum over d of q[d] key[t][d],  p = hb_relu(s) on the slice [k, m),  out[d] = (sum over t of p[t] value[t][d]) / length
+ * for the t < length of a sequence, whose token t lies in page page_table[b][t / page] (DEVICE int32, batch x table_width) at offset t mod page.  Query
+ * head h reads head h / (q_heads / heads) of the cache.  lens: DEVICE int32 per sequence, taken as 0 below 0 and as max_len above it; a
+ * sequence of length 0 gets shares 0 and 0.  A position whose page is out of range is a hole: it takes part in nothing but the length.
+ * The division: o = sum truncated by 16 + e, e = floor(log2 length); out = o times floor((2^(16+e) + floor(length / 2)) / length), truncated by 16.
+ * q0, q1, out0, out1: batch x q_heads x dim.  q_heads: a multiple of heads.  table_width * page >= max_len.
+ * Dealer material, with S_j = hb_tensor_seed(seed, j), row = b * q_heads + head, i = row * dim + d, j = row * max_len + t: masks of the query
+ * words 2i, 2i + 1 of the stream started at S_0; score j words 5j .. 5j + 4 of S_1 (c_0, then the truncation's); the ReLU is hb_relu's on the
+ * tensor batch x q_heads x max_len of scores with seed S_2, shares 0 and 0 behind a sequence's end and in holes; masks of p words 2j, 2j + 1
+ * of S_3; output i words 9i .. 9i + 8 of S_4 (c_0, first and second truncation).  A product's party shares, with a the fresh mask, b the cache's, eps =
+ * x - a opened now and D = y - b: c_0 + sum eps (b_0 + D) + D a_0 and (sum a b - c_0) + sum eps b_1 + D a_1.
+ * workspace: DEVICE, 256-byte aligned, hb_attention_workspace_bytes(cache, batch, q_heads, max_len) bytes (0 for invalid sizes; of `cache` the sizes
+ * count), overlapping nothing; contents before and after mean nothing; calls that may overlap in time need one each.  batch <= 65535.
+ * opened_bits receives 192 batch q_heads dim + n (128 + hb_opened_bits per element), n = batch q_heads max_len.
+ */
+HB_API int hb_attention(const hb_cache *cache, const int64_t *q0, const int64_t *q1, size_t batch, int q_heads, const int32_t *page_table,
+                        size_t table_width, const int32_t *lens, size_t max_len, int k, int m, uint64_t seed, int64_t *out0, int64_t *out1,
+                        void *workspace, size_t workspace_bytes, uint64_t *opened_bits, void *stream);
+HB_API size_t hb_attention_workspace_bytes(const hb_cache *cache, size_t batch, int q_heads, size_t max_len);
+
 /* Seed of tensor `tensor_id` in a set of tensors keyed by one root seed (host-only, no GPU work). */
 HB_API uint64_t hb_tensor_seed(uint64_t root_seed, uint64_t tensor_id);
 

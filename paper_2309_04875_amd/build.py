@@ -82,7 +82,7 @@ def build(verbose: bool = False, jobs: int = 0) -> str:
     work = tempfile.mkdtemp(prefix="hb_build_")
     try:
         probes = (os.path.join(CSRC, "hb_probes.hip"), os.path.join(work, "hb_probes.o"), [])
-        units = [(os.path.join(CSRC, "hb_api.hip"), os.path.join(work, "hb_api.o"), [])]
+        units = [(os.path.join(CSRC, name + ".hip"), os.path.join(work, name + ".o"), []) for name in ("hb_api", "hb_linear", "hb_attention")]
         for mode in MODES:
             for lo, hi in WIDTH_RANGES:
                 units.append((os.path.join(CSRC, "hb_launch_part.hip"),

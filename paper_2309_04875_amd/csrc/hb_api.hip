@@ -13,6 +13,7 @@
 #include <utility>
 #include <vector>
 
+#include "hb_check.hpp"
 #include "hb_eco.hpp"
 #include "hb_float.hpp"
 #include "hb_kernels.hpp"
@@ -21,15 +22,29 @@
 #include "hb_party.hpp"
 
 namespace {
-
 thread_local char g_hip_error[256] = "";
+}  // namespace
 
+namespace hb {
 int fail_hip(hipError_t e, const char *what)
 {
     std::snprintf(g_hip_error, sizeof(g_hip_error), "%s: %s", what, hipGetErrorString(e));
     (void)hipGetLastError();
     return HB_EHIP;
 }
+}  // namespace hb
+
+namespace {
+
+using hb::KnownAllocations;
+using hb::Range;
+using hb::check_common;
+using hb::check_device_buffer;
+using hb::check_float_buffer;
+using hb::disjoint;
+using hb::fail_hip;
+using hb::range_of;
+using hb::same;
 
 // No C++ exception leaves an entry point: what can throw here is the host memory of a set's launches.
 template <class Body>
@@ -45,93 +60,6 @@ int no_throw(const Body &body)
 bool valid_slice(int k, int m) { return k >= 0 && m > k && m <= 64; }
 
 int rounds_of(int w) { return hb::ceil_log2(w); }
-
-struct Range {
-    uintptr_t lo, hi;
-};
-
-Range range_of(const void *p, size_t n) { return Range{(uintptr_t)p, (uintptr_t)p + n * sizeof(int64_t)}; }
-
-bool same(Range a, Range b) { return a.lo == b.lo; }
-bool disjoint(Range a, Range b) { return a.hi <= b.lo || b.hi <= a.lo; }
-
-// Allocations that the checks of ONE call have found to be this GPU's memory.  The buffers of a call mostly lie in a few
-// allocations (a framework's allocator cuts many tensors out of one), and two queries of the HIP runtime for each of them
-// were 0.2 us a buffer: 0.8 us of a call on one tensor, 12 us of one on 17.  Nothing is kept after the call.
-struct KnownAllocations {
-    static constexpr int kMost = 16;
-    Range at[kMost];
-    unsigned found = 0;                  // the newest kMost are kept
-    int device = -1;                     // current device, once asked for
-};
-
-// The buffer must be memory the GPU can address, and [p, p + bytes) must lie inside one allocation.
-int check_device_bytes(const void *p, size_t bytes, KnownAllocations &known)
-{
-    const Range r{(uintptr_t)p, (uintptr_t)p + bytes};
-    for (unsigned i = 0; i < known.found && i < (unsigned)KnownAllocations::kMost; ++i) {
-        const Range &a = known.at[i];
-        if (r.lo >= a.lo && r.lo < a.hi) return r.hi <= a.hi ? HB_OK : HB_EINVAL;
-    }
-    hipPointerAttribute_t attr;
-    hipError_t e = hipPointerGetAttributes(&attr, p);
-    if (e != hipSuccess) {
-        (void)hipGetLastError();
-        return HB_EINVAL;  // not known to the HIP runtime: plain host memory or a wild pointer
-    }
-    switch (attr.type) {
-    case hipMemoryTypeDevice:     // memory of another GPU is not addressable from the kernels launched here
-        if ((known.device < 0 && hipGetDevice(&known.device) != hipSuccess) || attr.device != known.device) {
-            (void)hipGetLastError();
-            return HB_EINVAL;
-        }
-        break;
-    case hipMemoryTypeManaged:
-        break;
-    case hipMemoryTypeHost:  // pinned host memory is usable only through its device-side address
-        if (attr.devicePointer != p) return HB_EINVAL;
-        break;
-    default:  // unregistered host memory, arrays
-        return HB_EINVAL;
-    }
-    hipDeviceptr_t base = nullptr;
-    size_t size = 0;
-    e = hipMemGetAddressRange(&base, &size, (hipDeviceptr_t)p);
-    if (e != hipSuccess) {
-        (void)hipGetLastError();
-        return HB_OK;  // allocation kinds without a queryable range: the attribute check has passed
-    }
-    const Range a{(uintptr_t)base, (uintptr_t)base + size};
-    if (attr.type == hipMemoryTypeDevice) known.at[known.found++ % KnownAllocations::kMost] = a;
-    return (r.lo >= a.lo && r.hi <= a.hi) ? HB_OK : HB_EINVAL;
-}
-
-int check_device_buffer(const void *p, size_t n, KnownAllocations &known) { return check_device_bytes(p, n * sizeof(int64_t), known); }
-
-int check_common(const void *const *ptrs, int count, size_t n, KnownAllocations &known)
-{
-    if (n > HB_MAX_ELEMENTS) return HB_EINVAL;
-    if (n == 0) return HB_OK;
-    for (int i = 0; i < count; ++i) {
-        if (ptrs[i] == nullptr) return HB_EINVAL;
-    }
-    for (int i = 0; i < count; ++i) {
-        if (((uintptr_t)ptrs[i] & 7u) != 0) return HB_EALIGN;
-    }
-    for (int i = 0; i < count; ++i) {
-        const int st = check_device_buffer(ptrs[i], n, known);
-        if (st != HB_OK) return st;
-    }
-    return HB_OK;
-}
-
-// A device buffer of n floats with the given alignment.
-int check_float_buffer(const void *p, size_t n, unsigned align, KnownAllocations &known)
-{
-    if (p == nullptr) return HB_EINVAL;
-    if (((uintptr_t)p & (align - 1)) != 0) return HB_EALIGN;
-    return check_device_bytes(p, n * sizeof(float), known);
-}
 
 bool all_aligned16(const void *const *ptrs, int count)
 {

@@ -1,0 +1,203 @@
+// C ABI of the paged cache and its attention: argument checks, launches on the caller's stream.
+#include "hb_attention.hpp"
+#include "hb_check.hpp"
+#include "hb_launch.hpp"
+
+namespace {
+
+// What a cache has to be, whatever is done with it.
+int check_cache(const hb_cache *cache)
+{
+    if (cache == nullptr) return HB_EINVAL;
+    if (cache->heads < 1 || cache->heads > 4096 || cache->page < 1 || cache->page > 65536 || cache->dim < 2 || cache->dim > HB_CACHE_MAX_DIM ||
+        cache->dim % 2 != 0)
+        return HB_EINVAL;
+    if (cache->pages > ((size_t)1 << 31) - 1) return HB_EINVAL;
+    const size_t tokens = cache->pages * (size_t)cache->page;             // below 2^48
+    return tokens * (size_t)cache->heads <= HB_MAX_ELEMENTS / (size_t)cache->dim ? HB_OK : HB_EINVAL;
+}
+
+size_t cache_bytes(const hb_cache *cache) { return 8 * cache->pages * (size_t)cache->heads * (size_t)cache->page * (size_t)cache->dim; }
+
+hb::CacheView view_of(const hb_cache *cache)
+{
+    hb::CacheView c = {};
+    c.keys = (uint64_t *)cache->keys;
+    c.values = (uint64_t *)cache->values;
+    c.page_seeds = cache->page_seeds;
+    c.pages = (uint32_t)cache->pages;
+    c.heads = (uint32_t)cache->heads;
+    c.page = (uint32_t)cache->page;
+    c.dim = (uint32_t)cache->dim;
+    return c;
+}
+
+size_t round_up(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// Workspace of hb_attention: shares of the scores, then the splits' partial sums.
+struct AttentionLayout {
+    size_t scores1, parts, bytes;
+    uint32_t splits, per_split;
+};
+
+bool attention_sizes(const hb_cache *cache, size_t batch, int q_heads, size_t max_len)
+{
+    return check_cache(cache) == HB_OK && q_heads >= cache->heads && q_heads <= 65536 && q_heads % cache->heads == 0 && batch <= 65535 &&
+           max_len <= ((size_t)1 << 30) && batch * q_heads * max_len <= HB_MAX_ELEMENTS;
+}
+
+AttentionLayout attention_layout(const hb_cache *cache, size_t batch, int q_heads, size_t max_len)
+{
+    AttentionLayout lay = {};
+    const size_t scores = round_up(8 * batch * q_heads * max_len), numbers = batch * q_heads * cache->dim;
+    lay.per_split = 256;
+    lay.splits = (uint32_t)((max_len + lay.per_split - 1) / lay.per_split);
+    while (lay.splits > 64) {
+        lay.per_split *= 2;
+        lay.splits = (uint32_t)((max_len + lay.per_split - 1) / lay.per_split);
+    }
+    lay.scores1 = scores;
+    lay.parts = 2 * scores;
+    lay.bytes = 2 * scores + round_up(16 * numbers * lay.splits);
+    return lay;
+}
+
+}  // namespace
+
+extern "C" {
+
+int hb_cache_append(const hb_cache *cache, const int64_t *k0, const int64_t *k1, const int64_t *v0, const int64_t *v1, size_t tokens,
+                    const int64_t *slots, const int32_t *positions, const int32_t *cos, const int32_t *sin, size_t table_rows, int rot, int frac,
+                    const int64_t *q0, const int64_t *q1, int q_heads, int32_t q_mul, uint64_t seed, int64_t *q_out0, int64_t *q_out1,
+                    uint64_t *opened_bits, void *stream)
+{
+    int st = check_cache(cache);
+    if (st != HB_OK) return st;
+    if (rot < 0 || rot > cache->dim || rot % 2 != 0 || frac < 1 || frac > 30 || q_heads < 0 || q_heads > 65536) return HB_EINVAL;
+    if (tokens > HB_LINEAR_MAX || table_rows > ((size_t)1 << 31) - 1) return HB_EINVAL;
+    const size_t row = 8 * tokens * (size_t)cache->dim, kv = row * cache->heads, q = row * q_heads, table = 4 * table_rows * (size_t)(rot / 2);
+    if (tokens != 0) {
+        if (rot != 0 && table_rows == 0) return HB_EINVAL;
+        const size_t store = cache_bytes(cache);
+        const void *ptrs[15] = {cache->keys, cache->values, q_out0, q_out1, cache->page_seeds, k0, k1, v0, v1, slots, positions, cos, sin, q0, q1};
+        const size_t sizes[15] = {store, store, q, q, 8 * cache->pages, kv, kv, kv, kv, 8 * tokens, rot != 0 ? 4 * tokens : 0, table, table, q, q};
+        const unsigned align[15] = {8, 8, 8, 8, 8, 8, 8, 8, 8, 8, 4, 4, 4, 8, 8};
+        st = hb::check_buffers(ptrs, sizes, align, 15);
+        if (st != HB_OK) return st;
+        // the rotated queries may replace the queries; every other overlap of what is written is refused
+        if (!hb::outputs_disjoint(ptrs, sizes, 13, 0, 4)) return HB_EINVAL;
+        for (int o = 0; o < 4 && q != 0; ++o) {
+            for (int i = 13; i < 15; ++i) {
+                const hb::Range a{(uintptr_t)ptrs[o], (uintptr_t)ptrs[o] + sizes[o]}, b{(uintptr_t)ptrs[i], (uintptr_t)ptrs[i] + sizes[i]};
+                if (sizes[o] != 0 && !hb::disjoint(a, b) && !(o >= 2 && hb::same(a, b))) return HB_EINVAL;
+            }
+        }
+        hb::AppendArgs a = {};
+        a.cache = view_of(cache);
+        const int64_t *const in[6] = {k0, k1, v0, v1, q0, q1};
+        for (int p = 0; p < 2; ++p) {
+            a.k[p] = (const uint64_t *)in[p];
+            a.v[p] = (const uint64_t *)in[2 + p];
+            a.q[p] = (const uint64_t *)in[4 + p];
+        }
+        a.qo[0] = (uint64_t *)q_out0;
+        a.qo[1] = (uint64_t *)q_out1;
+        a.slots = slots;
+        a.positions = positions;
+        a.cos = cos;
+        a.sin = sin;
+        a.tokens = tokens;
+        a.table_rows = table_rows;
+        a.seedA = hb::stream_word(seed, 1);
+        a.q_heads = (uint32_t)q_heads;
+        a.rot = (uint32_t)rot;
+        a.frac = frac;
+        a.q_mul = q_mul;
+        const uint64_t items = (2 * (uint64_t)cache->heads + q_heads) * (cache->dim / 2) * tokens;
+        const uint64_t blocks = (items + hb::kAppendBlock - 1) / hb::kAppendBlock;
+        if (blocks > 0x7fffffffull) return HB_EINVAL;
+        hipLaunchKernelGGL(hb::cache_append_kernel, dim3((unsigned)blocks), dim3(hb::kAppendBlock), 0, (hipStream_t)stream, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return hb::fail_hip(e, "kernel launch");
+    }
+    if (opened_bits) *opened_bits = 64ull * tokens * ((uint64_t)cache->heads * (rot + 2 * cache->dim) + (uint64_t)q_heads * cache->dim);
+    return HB_OK;
+}
+
+size_t hb_attention_workspace_bytes(const hb_cache *cache, size_t batch, int q_heads, size_t max_len)
+{
+    return attention_sizes(cache, batch, q_heads, max_len) ? attention_layout(cache, batch, q_heads, max_len).bytes : 0;
+}
+
+int hb_attention(const hb_cache *cache, const int64_t *q0, const int64_t *q1, size_t batch, int q_heads, const int32_t *page_table,
+                 size_t table_width, const int32_t *lens, size_t max_len, int k, int m, uint64_t seed, int64_t *out0, int64_t *out1,
+                 void *workspace, size_t workspace_bytes, uint64_t *opened_bits, void *stream)
+{
+    if (!attention_sizes(cache, batch, q_heads, max_len) || !(k >= 0 && m > k && m <= 64)) return HB_EINVAL;
+    if (table_width > ((size_t)1 << 31) - 1 || table_width * cache->page < max_len) return HB_EINVAL;
+    const size_t scores = batch * q_heads * max_len;
+    const uint64_t bits = 64ull * batch * q_heads * cache->dim * 3 + hb_opened_bits(1, k, m, scores) + 128ull * scores;
+    if (batch != 0) {
+        const AttentionLayout lay = attention_layout(cache, batch, q_heads, max_len);
+        if (workspace_bytes < lay.bytes) return HB_EINVAL;
+        const size_t q = 8 * batch * q_heads * cache->dim, store = max_len != 0 ? cache_bytes(cache) : 0;
+        const void *ptrs[10] = {out0, out1, workspace, q0, q1, cache->keys, cache->values, cache->page_seeds, page_table, lens};
+        const size_t sizes[10] = {q, q, lay.bytes, q, q, store, store, max_len != 0 ? 8 * cache->pages : 0, 4 * batch * table_width, 4 * batch};
+        const unsigned align[10] = {8, 8, 256, 8, 8, 8, 8, 8, 4, 4};
+        const int st = hb::check_buffers(ptrs, sizes, align, 10);
+        if (st != HB_OK) return st;
+        if (!hb::outputs_disjoint(ptrs, sizes, 10, 0, 3)) return HB_EINVAL;
+        hb::AttentionArgs a = {};
+        a.cache = view_of(cache);
+        a.q[0] = (const uint64_t *)q0;
+        a.q[1] = (const uint64_t *)q1;
+        a.out[0] = (uint64_t *)out0;
+        a.out[1] = (uint64_t *)out1;
+        char *base = (char *)workspace;
+        a.scores[0] = (uint64_t *)base;
+        a.scores[1] = (uint64_t *)(base + lay.scores1);
+        a.parts = (uint64_t *)(base + lay.parts);
+        a.table = page_table;
+        a.lens = lens;
+        a.table_width = table_width;
+        a.seed_q = hb_tensor_seed(seed, 0);
+        a.seed_s = hb_tensor_seed(seed, 1);
+        const uint64_t seed_relu = hb_tensor_seed(seed, 2);
+        a.seed_p = hb_tensor_seed(seed, 3);
+        a.seed_o = hb_tensor_seed(seed, 4);
+        a.batch = (uint32_t)batch;
+        a.q_heads = (uint32_t)q_heads;
+        a.max_len = (uint32_t)max_len;
+        a.splits = lay.splits;
+        a.per_split = lay.per_split;
+        const hb::GroupLauncher relu = hb::launcher_table().f[hb::kRelu][m - k - 1];
+        if (relu == nullptr) return hb::fail_hip(hipErrorInvalidDeviceFunction, "no kernel was built for this slice width");
+        hipError_t e = hipSuccess;
+        const dim3 block(hb::kAttentionBlock);
+        if (max_len != 0) {
+            const uint64_t blocks = (scores + hb::kAttentionBlock / 64 - 1) / (hb::kAttentionBlock / 64);
+            if (blocks > 0x7fffffffull) return HB_EINVAL;
+            hipLaunchKernelGGL(hb::attention_scores_kernel, dim3((unsigned)blocks), block, 0, (hipStream_t)stream, a);
+            e = hipGetLastError();
+            if (e == hipSuccess) {
+                e = relu(a.scores[0], a.scores[1], scores, k, hb::stream_word(seed_relu, 0), hb::stream_word(seed_relu, 1), a.scores[0], a.scores[1],
+                         (hipStream_t)stream);
+            }
+            if (e == hipSuccess) {
+                const uint64_t over = ((uint64_t)batch * q_heads * cache->dim + hb::kAttentionBlock - 1) / hb::kAttentionBlock;
+                hipLaunchKernelGGL(hb::attention_values_kernel, dim3((unsigned)over, lay.splits), block, 0, (hipStream_t)stream, a);
+                e = hipGetLastError();
+            }
+        }
+        if (e == hipSuccess) {
+            const unsigned over = (unsigned)(((uint64_t)q_heads * cache->dim + hb::kAttentionBlock - 1) / hb::kAttentionBlock);
+            hipLaunchKernelGGL(hb::attention_join_kernel, dim3(over, (unsigned)batch), block, 0, (hipStream_t)stream, a);
+            e = hipGetLastError();
+        }
+        if (e != hipSuccess) return hb::fail_hip(e, "kernel launch");
+    }
+    if (opened_bits) *opened_bits = bits;
+    return HB_OK;
+}
+
+}  // extern "C"

@@ -29,6 +29,7 @@ EXPORTS = ("hb_drelu", "hb_relu", "hb_sign_shares", "hb_open", "hb_relu_batch", 
            "hb_share_f32", "hb_reveal_f32", "hb_sim_relu_f32", "hb_relu_party", "hb_relu_party_ex", "hb_party_workspace_bytes_ex", "hb_party_wire_words_ex", "hb_party_wire_offset_ex", "hb_relu_party_static", "hb_party_workspace_bytes", "hb_party_wire_words", "hb_party_wire_offset",
            "hb_drelu_ex", "hb_relu_ex", "hb_relu_batch_ex", "hb_drelu_batch_ex", "hb_plan_create", "hb_plan_run", "hb_plan_destroy",
            "hb_drelu_mp", "hb_relu_mp", "hb_opened_bits_mp",
+           "hb_linear_q4", "hb_cache_append", "hb_attention", "hb_attention_workspace_bytes",
            "hb_tensor_seed",
            "hb_opened_bits", "hb_opened_bits_ex", "hb_strerror", "hb_last_hip_error")
 
@@ -62,6 +63,12 @@ class hb_tensor(ctypes.Structure):
     _fields_ = [("share0", ctypes.c_void_p), ("share1", ctypes.c_void_p), ("out0", ctypes.c_void_p),
                 ("out1", ctypes.c_void_p), ("n", ctypes.c_size_t), ("k", ctypes.c_int), ("m", ctypes.c_int),
                 ("seed", ctypes.c_uint64)]
+
+
+class hb_cache(ctypes.Structure):
+    """Mirror of `struct hb_cache` in include/hb.h."""
+    _fields_ = [("keys", ctypes.c_void_p), ("values", ctypes.c_void_p), ("page_seeds", ctypes.c_void_p), ("pages", ctypes.c_size_t),
+                ("heads", ctypes.c_int), ("page", ctypes.c_int), ("dim", ctypes.c_int)]
 
 
 class HbError(RuntimeError):
@@ -141,6 +148,15 @@ def load():
     lib.hb_eco_choose.argtypes = [u64p]
     lib.hb_open.restype = ci
     lib.hb_open.argtypes = [vp, vp, sz, ci, vp, vp]
+    lib.hb_linear_q4.restype = ci
+    lib.hb_linear_q4.argtypes = [vp, vp, sz, sz, sz, vp, vp, ci, ci, u64, vp, vp, u64p, vp]
+    cachep = ctypes.POINTER(hb_cache)
+    lib.hb_cache_append.restype = ci
+    lib.hb_cache_append.argtypes = [cachep, vp, vp, vp, vp, sz, vp, vp, vp, vp, sz, ci, ci, vp, vp, ci, ctypes.c_int32, u64, vp, vp, u64p, vp]
+    lib.hb_attention.restype = ci
+    lib.hb_attention.argtypes = [cachep, vp, vp, sz, ci, vp, sz, vp, sz, ci, ci, u64, vp, vp, vp, sz, u64p, vp]
+    lib.hb_attention_workspace_bytes.restype = sz
+    lib.hb_attention_workspace_bytes.argtypes = [cachep, sz, ci, sz]
     lib.hb_tensor_seed.restype = u64
     lib.hb_tensor_seed.argtypes = [u64, u64]
     lib.hb_opened_bits.restype = u64
@@ -589,6 +605,112 @@ def hb_open(share0, share1, binary=False, out=None, stream=None):
     _check(load().hb_open(share0.data_ptr(), share1.data_ptr(), n, int(bool(binary)), out.data_ptr(),
                           _stream_handle(stream)))
     return out
+
+
+def _typed(t, dtype, *shape):
+    """Address of a contiguous CUDA tensor of the given type and shape (None: any size there)."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+        raise TypeError("expected a contiguous %s CUDA tensor" % str(dtype).replace("torch.", ""))
+    if t.dim() != len(shape) or any(want is not None and have != want for have, want in zip(t.shape, shape)):
+        raise ValueError("expected shape %s, got %s" % (tuple("any" if n is None else n for n in shape), tuple(t.shape)))
+    return t.data_ptr()
+
+
+def hb_linear_q4(x0, x1, weight, scales, group, frac, seed, out0=None, out1=None, stream=None):
+    """Linear layer on shares with public 4-bit weights: x [..., in], weight uint8 [out, (in + 1) // 2], scales int32
+    [out, ceil(in / group)] at 2^frac; returns (out0, out1, opened_bits), outputs [..., out]."""
+    import torch
+    if not isinstance(x0, torch.Tensor) or not isinstance(weight, torch.Tensor):
+        raise TypeError("expected CUDA tensors")
+    group = int(group)
+    inputs, outputs = x0.shape[-1] if x0.dim() else 0, weight.shape[0] if weight.dim() else 0
+    if inputs < 1 or group < 1:
+        raise ValueError("a linear layer has inputs, and groups of them")
+    if out0 is None:
+        out0 = torch.empty(x0.shape[:-1] + (outputs,), dtype=torch.int64, device=x0.device)
+    if out1 is None:
+        out1 = torch.empty(x0.shape[:-1] + (outputs,), dtype=torch.int64, device=x0.device)
+    lead = tuple(x0.shape[:-1])
+    at = [_typed(x0, torch.int64, *lead, inputs), _typed(x1, torch.int64, *lead, inputs), _typed(weight, torch.uint8, outputs, (inputs + 1) // 2),
+          _typed(scales, torch.int32, outputs, -(-inputs // group)), _typed(out0, torch.int64, *lead, outputs), _typed(out1, torch.int64, *lead, outputs)]
+    bits = ctypes.c_uint64(0)
+    _check(load().hb_linear_q4(at[0], at[1], x0.numel() // inputs, inputs, outputs, at[2], at[3], group, int(frac), int(seed) & (2**64 - 1), at[4],
+                               at[5], ctypes.byref(bits), _stream_handle(stream)))
+    return out0, out1, int(bits.value)
+
+
+class Cache:
+    """A paged cache (struct hb_cache): keys, values int64 [pages, heads, tokens per page, dim], page_seeds int64 [pages]; keeps the tensors."""
+
+    def __init__(self, keys, values, page_seeds):
+        import torch
+        at = _typed(keys, torch.int64, None, None, None, None), _typed(values, torch.int64, *keys.shape), _typed(page_seeds, torch.int64, keys.shape[0])
+        self.keys, self.values, self.page_seeds = keys, values, page_seeds
+        self.pages, self.heads, self.page, self.dim = keys.shape
+        self.struct = hb_cache(*at, *keys.shape)
+        self.pointer = ctypes.byref(self.struct)
+
+
+def _cache_arg(cache):
+    if not isinstance(cache, Cache):
+        raise TypeError("expected a Cache")
+    return cache.pointer
+
+
+def hb_cache_append(cache, k0, k1, v0, v1, slots, positions, cos, sin, frac, seed, q0=None, q1=None, q_mul=0, q_out0=None, q_out1=None,
+                    stream=None):
+    """Append keys and values [tokens, heads, dim] at slots (int64 [tokens], out of range: padding), keys and queries [tokens, q_heads, dim] rotated
+    by rows positions (int32 [tokens]) of cos and sin (int32 [rows, rot / 2] at 2^frac; all three None: no rotation), queries times q_mul / 2^frac;
+    returns (q_out0, q_out1, opened_bits), the outputs None without queries."""
+    import torch
+    pointer = _cache_arg(cache)
+    tokens = slots.shape[0] if isinstance(slots, torch.Tensor) and slots.dim() else 0
+    kv = [_typed(t, torch.int64, tokens, cache.heads, cache.dim) for t in (k0, k1, v0, v1)]
+    rows, half, turn = 0, 0, [None, None, None]
+    if cos is not None or sin is not None or positions is not None:
+        rows, half = cos.shape if isinstance(cos, torch.Tensor) and cos.dim() == 2 else (None, None)
+        turn = [_typed(positions, torch.int32, tokens), _typed(cos, torch.int32, None, None), _typed(sin, torch.int32, rows, half)]
+    heads, q = 0, [None, None, None, None]
+    if q0 is not None or q1 is not None:
+        heads = q0.shape[1] if isinstance(q0, torch.Tensor) and q0.dim() == 3 else None
+        if q_out0 is None:
+            q_out0 = torch.empty_like(q0)
+        if q_out1 is None:
+            q_out1 = torch.empty_like(q1)
+        q = [_typed(t, torch.int64, tokens, heads, cache.dim) for t in (q0, q1, q_out0, q_out1)]
+    bits = ctypes.c_uint64(0)
+    _check(load().hb_cache_append(pointer, *kv, tokens, _typed(slots, torch.int64, tokens), *turn, rows, 2 * half, int(frac), q[0], q[1], heads,
+                                  int(q_mul), int(seed) & (2**64 - 1), q[2], q[3], ctypes.byref(bits), _stream_handle(stream)))
+    return q_out0, q_out1, int(bits.value)
+
+
+def hb_attention_workspace_bytes(cache, batch, q_heads, max_len):
+    return int(load().hb_attention_workspace_bytes(_cache_arg(cache), int(batch), int(q_heads), int(max_len)))
+
+
+def hb_attention(cache, q0, q1, page_table, lens, max_len, k, m, seed, out0=None, out1=None, workspace=None, stream=None):
+    """Attention of one new token per sequence, q [batch, q_heads, dim], over the cache's pages page_table (int32 [batch, width]) up to lens (int32
+    [batch]), with ReLU on the slice [k, m) of the scores; returns (out0, out1, opened_bits).  workspace: a uint8 CUDA tensor, allocated here
+    unless one is passed."""
+    import torch
+    pointer = _cache_arg(cache)
+    if out0 is None:
+        out0 = torch.empty_like(q0)
+    if out1 is None:
+        out1 = torch.empty_like(q1)
+    at = [_typed(q0, torch.int64, None, None, cache.dim)]
+    batch, heads = q0.shape[:2]
+    at += [_typed(t, torch.int64, batch, heads, cache.dim) for t in (q1, out0, out1)]
+    at += [_typed(page_table, torch.int32, batch, None), _typed(lens, torch.int32, batch)]
+    if workspace is None:
+        need = int(load().hb_attention_workspace_bytes(pointer, batch, heads, int(max_len)))
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q0.device)
+    room = _typed(workspace, torch.uint8, None)
+    bits = ctypes.c_uint64(0)
+    _check(load().hb_attention(pointer, at[0], at[1], batch, heads, at[4], page_table.shape[1], at[5], int(max_len), int(k), int(m),
+                               int(seed) & (2**64 - 1), at[2], at[3], room, workspace.numel(), ctypes.byref(bits), _stream_handle(stream)))
+    return out0, out1, int(bits.value)
 
 
 def hb_tensor_seed(root_seed, tensor_id):
