@@ -280,7 +280,8 @@ HB_API int hb_eco_choose(const uint64_t *counts);
  *   t_1 = g ((r >> 63) - v_3) - (((r mod 2^63) >> f) - v_2).
  * t_0 + t_1 is floor(y / 2^f), or one more where the lower f bits of y and r carry.  Outside the stated range the result is unspecified.
  */
-#define HB_LINEAR_MAX ((size_t)1 << 24)   /* most rows, inputs, outputs and tokens of one call */
+#define HB_LINEAR_MAX ((size_t)1 << 24)   /* most rows, outputs and tokens of one call */
+#define HB_LINEAR_MAX_IN ((size_t)1 << 17)
 #define HB_CACHE_MAX_DIM 256
 
 /*
@@ -289,7 +290,7 @@ HB_API int hb_eco_choose(const uint64_t *counts);
  * weight: DEVICE, out x ceil(in / 2) bytes; byte j of a row holds inputs 2j (lower four bits) and 2j + 1, as numbers in -8 .. 7 in two's
  * complement; the upper half of a last byte that no input has is not used.  scales: DEVICE, out x ceil(in / group) int32 S = round(2^frac s),
  * 4-byte aligned.  group: a positive multiple of 32; frac: 1 .. 31.  x0, x1: rows x in; out0, out1: rows x out; 8-byte aligned, the outputs
- * overlapping nothing.  in >= 1; rows == 0 or out == 0 is a successful no-op.
+ * overlapping nothing.  in: 1 .. HB_LINEAR_MAX_IN; rows == 0 or out == 0 is a successful no-op.
  * Dealer words of output i = r * out + n: A[4i .. 4i+3], A the arithmetic stream of `seed` (the one of hb_relu: give every call its own seed).
  * opened_bits receives 64 rows out.
  */

@@ -1,0 +1,63 @@
+// Sums of products on Z_2^64 by the matrix cores: numbers of the ring as eight digits of eight bits.
+//
+// x = sum over i of s_i 2^(8i) mod 2^64 with signed digits -128 .. 127, one for each multiplicand of an int8 matrix instruction, whose int32 sums
+// are exact: the bytes of x + 0x8080808080808080, each less 128 (the addition carries what a digit of 128 and more owes to the next; the
+// last carry leaves the ring).  Less 128 is the top bit flipped, for a byte read as signed.
+#pragma once
+
+#include "hb_fixed.hpp"
+
+namespace hb {
+
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
+typedef int i32x2_t __attribute__((ext_vector_type(2)));
+
+constexpr uint64_t kDigitBias = 0x8080808080808080ull;
+constexpr uint32_t kDigitFlip = 0x80808080u;
+
+// The 4 x 4 bytes of four words turned: word j gets byte j of each.
+__device__ __forceinline__ void turn_bytes(const uint32_t (&w)[4], uint32_t *out)
+{
+    const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), b = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u);
+    const uint32_t c = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u), d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+    out[0] = __builtin_amdgcn_perm(c, a, 0x05040100u);
+    out[1] = __builtin_amdgcn_perm(c, a, 0x07060302u);
+    out[2] = __builtin_amdgcn_perm(d, b, 0x05040100u);
+    out[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
+}
+
+// Digits of four numbers: out[i] holds digit i of v[0] .. v[3], one byte each.
+__device__ __forceinline__ void digits_of(const uint64_t (&v)[4], uint32_t (&out)[8])
+{
+    uint32_t low[4], high[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint64_t x = v[j] + kDigitBias;
+        low[j] = (uint32_t)x;
+        high[j] = (uint32_t)(x >> 32);
+    }
+    turn_bytes(low, out);
+    turn_bytes(high, out + 4);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) out[i] ^= kDigitFlip;
+}
+
+// c + A B of 16 x 64 by 64 x 16 int8.  Lane l holds 16 numbers of row (A) or column (B) l mod 16 in each of its four registers' bytes, those of
+// the same 16 places of the sum in A and B (lanes l with the same l / 16 share them); which places is the caller's choice.  The result's lane l
+// holds rows 4 (l / 16) .. + 3 of column l mod 16.
+__device__ __forceinline__ i32x4_t mfma_16x16x64(i32x4_t a, i32x4_t b, i32x4_t c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
+// The same of 32 places, eight a lane.
+__device__ __forceinline__ i32x4_t mfma_16x16x32(i32x2_t a, i32x2_t b, i32x4_t c)
+{
+    return __builtin_amdgcn_mfma_i32_16x16x32_i8(__builtin_bit_cast(long, a), __builtin_bit_cast(long, b), c, 0, 0, 0);
+}
+
+// What a lane has written to LDS and other lanes of its wavefront read.
+__device__ __forceinline__ void wave_exchange()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+}  // namespace hb

@@ -2,12 +2,44 @@
 #include "hb_check.hpp"
 #include "hb_linear.hpp"
 
+namespace {
+
+template <int TM, int RT, int WN, int WK, int FLUSH>
+hipError_t go(hb::LinearArgs &a, hipStream_t stream)
+{
+    const uint64_t tiles = ((uint64_t)a.outs + 16 * WN * RT - 1) / (16 * WN * RT);
+    a.row_tiles = (a.rows + TM - 1) / TM;
+    const uint64_t blocks = tiles * a.row_tiles;
+    if (blocks > 0x7fffffffull) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((hb::linear_q4_kernel<TM, RT, WN, WK, FLUSH>), dim3((unsigned)blocks), dim3(64 * WN * WK), 0, stream, a);
+    return hipGetLastError();
+}
+
+template <int FLUSH>
+hipError_t by_shape(hb::LinearArgs &a, hipStream_t stream)
+{
+    const uint64_t wide = ((uint64_t)a.outs + 255) / 256 * ((a.rows + 3) / 4);
+    if (wide >= 512) return go<4, 4, 4, 1, FLUSH>(a, stream);
+    if (a.rows == 1) return go<1, 1, 1, 16, FLUSH>(a, stream);
+    if (a.rows == 2) return go<2, 1, 1, 8, FLUSH>(a, stream);
+    return go<4, 1, 1, 8, FLUSH>(a, stream);
+}
+
+hipError_t launch(hb::LinearArgs &a, uint64_t group, hipStream_t stream)
+{
+    if (group % 128 == 0) return by_shape<128>(a, stream);
+    if (group % 64 == 0) return by_shape<64>(a, stream);
+    return by_shape<32>(a, stream);
+}
+
+}  // namespace
+
 extern "C" int hb_linear_q4(const int64_t *x0, const int64_t *x1, size_t rows, size_t in, size_t out, const uint8_t *weight,
                             const int32_t *scales, int group, int frac, uint64_t seed, int64_t *out0, int64_t *out1,
                             uint64_t *opened_bits, void *stream)
 {
     if (group < 32 || group % 32 != 0 || frac < 1 || frac > 31) return HB_EINVAL;
-    if (in == 0 || in > HB_LINEAR_MAX || out > HB_LINEAR_MAX || rows > HB_LINEAR_MAX) return HB_EINVAL;
+    if (in == 0 || in > HB_LINEAR_MAX_IN || out > HB_LINEAR_MAX || rows > HB_LINEAR_MAX) return HB_EINVAL;
     const size_t groups = (in + group - 1) / group, row_bytes = (in + 1) / 2;
     if (rows != 0 && out != 0) {
         const size_t sizes[6] = {8 * rows * in, 8 * rows * in, 8 * rows * out, 8 * rows * out, out * row_bytes, 4 * out * groups};
@@ -17,6 +49,7 @@ extern "C" int hb_linear_q4(const int64_t *x0, const int64_t *x1, size_t rows, s
         if (st != HB_OK) return st;
         // outputs overlap nothing: other workgroups still read the inputs
         if (!hb::outputs_disjoint(ptrs, sizes, 6, 2, 4)) return HB_EINVAL;
+        const uint64_t a_group = (size_t)group < in ? group : (in + 127) / 128 * 128;      // one group: the last step's end is in it
         hb::LinearArgs a = {};
         a.x[0] = (const uint64_t *)x0;
         a.x[1] = (const uint64_t *)x1;
@@ -29,12 +62,10 @@ extern "C" int hb_linear_q4(const int64_t *x0, const int64_t *x1, size_t rows, s
         a.in = (uint32_t)in;
         a.outs = (uint32_t)out;
         a.groups = (uint32_t)groups;
-        a.group = group;
         a.frac = frac;
-        const uint64_t per = hb::kLinearBlock / 64, blocks = ((uint64_t)rows * out + per - 1) / per;
-        if (blocks > 0x7fffffffull) return HB_EINVAL;
-        hipLaunchKernelGGL(hb::linear_q4_kernel, dim3((unsigned)blocks), dim3(hb::kLinearBlock), 0, (hipStream_t)stream, a);
-        const hipError_t e = hipGetLastError();
+        a.weight_bytes = out * row_bytes;
+        a.group_inverse = ((1ull << 40) + a_group - 1) / a_group;
+        const hipError_t e = launch(a, a_group, (hipStream_t)stream);
         if (e != hipSuccess) return hb::fail_hip(e, "kernel launch");
     }
     if (opened_bits) *opened_bits = 64ull * rows * out;
