@@ -47,12 +47,12 @@ def _left(*args):
 
 class _NotLoaded:
     """The functions of `_binding`; until it is loaded each loads it and leaves the call to ctypes."""
-    shares = parties = batch = plan_run = sim_relu = share = reveal = eco_scan = party = staticmethod(_not_loaded)
+    shares = parties = batch = plan_run = sim_relu = share = reveal = eco_scan = party = linear = cache = append = attention = staticmethod(_not_loaded)
 
 
 class _NotThere:
     """The same where there is no `_binding`: every call is left to ctypes."""
-    shares = parties = batch = plan_run = sim_relu = share = reveal = eco_scan = party = staticmethod(_left)
+    shares = parties = batch = plan_run = sim_relu = share = reveal = eco_scan = party = linear = cache = append = attention = staticmethod(_left)
 
 
 _native = _NotLoaded
@@ -617,10 +617,26 @@ def _typed(t, dtype, *shape):
     return t.data_ptr()
 
 
+def _made_for(stream, make):
+    """What make() allocates, as memory of the stream that the call runs on: torch then gives none of it to another stream's tensors, or
+    theirs to it, before the work has ended."""
+    import torch
+    if stream is None:
+        return make()
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)))
+    with torch.cuda.stream(stream):
+        return make()
+
+
 def hb_linear_q4(x0, x1, weight, scales, group, frac, seed, out0=None, out1=None, stream=None):
     """Linear layer on shares with public 4-bit weights: x [..., in], weight uint8 [out, (in + 1) // 2], scales int32
     [out, ceil(in / group)] at 2^frac; returns (out0, out1, opened_bits), outputs [..., out]."""
     import torch
+    if stream is None:
+        done = _native.linear(x0, x1, weight, scales, group, frac, seed, out0, out1)
+        if done is not NotImplemented:
+            return done
     if not isinstance(x0, torch.Tensor) or not isinstance(weight, torch.Tensor):
         raise TypeError("expected CUDA tensors")
     group = int(group)
@@ -628,9 +644,9 @@ def hb_linear_q4(x0, x1, weight, scales, group, frac, seed, out0=None, out1=None
     if inputs < 1 or group < 1:
         raise ValueError("a linear layer has inputs, and groups of them")
     if out0 is None:
-        out0 = torch.empty(x0.shape[:-1] + (outputs,), dtype=torch.int64, device=x0.device)
+        out0 = _made_for(stream, lambda: torch.empty(x0.shape[:-1] + (outputs,), dtype=torch.int64, device=x0.device))
     if out1 is None:
-        out1 = torch.empty(x0.shape[:-1] + (outputs,), dtype=torch.int64, device=x0.device)
+        out1 = _made_for(stream, lambda: torch.empty(x0.shape[:-1] + (outputs,), dtype=torch.int64, device=x0.device))
     lead = tuple(x0.shape[:-1])
     at = [_typed(x0, torch.int64, *lead, inputs), _typed(x1, torch.int64, *lead, inputs), _typed(weight, torch.uint8, outputs, (inputs + 1) // 2),
           _typed(scales, torch.int32, outputs, -(-inputs // group)), _typed(out0, torch.int64, *lead, outputs), _typed(out1, torch.int64, *lead, outputs)]
@@ -644,18 +660,20 @@ class Cache:
     """A paged cache (struct hb_cache): keys, values int64 [pages, heads, tokens per page, dim], page_seeds int64 [pages]; keeps the tensors."""
 
     def __init__(self, keys, values, page_seeds):
-        import torch
-        at = _typed(keys, torch.int64, None, None, None, None), _typed(values, torch.int64, *keys.shape), _typed(page_seeds, torch.int64, keys.shape[0])
         self.keys, self.values, self.page_seeds = keys, values, page_seeds
-        self.pages, self.heads, self.page, self.dim = keys.shape
-        self.struct = hb_cache(*at, *keys.shape)
-        self.pointer = ctypes.byref(self.struct)
+        self.struct = _native.cache(keys, values, page_seeds)            # its bytes
+        if self.struct is NotImplemented:
+            import torch
+            at = _typed(keys, torch.int64, None, None, None, None), _typed(values, torch.int64, *keys.shape), _typed(page_seeds, torch.int64, keys.shape[0])
+            if max(keys.shape[1:]) >= 1 << 31:
+                raise ValueError("a cache's sizes are ints")
+            self.struct = bytes(hb_cache(*at, *keys.shape))
 
 
 def _cache_arg(cache):
     if not isinstance(cache, Cache):
         raise TypeError("expected a Cache")
-    return cache.pointer
+    return hb_cache.from_buffer_copy(cache.struct)
 
 
 def hb_cache_append(cache, k0, k1, v0, v1, slots, positions, cos, sin, frac, seed, q0=None, q1=None, q_mul=0, q_out0=None, q_out1=None,
@@ -664,7 +682,11 @@ def hb_cache_append(cache, k0, k1, v0, v1, slots, positions, cos, sin, frac, see
     by rows positions (int32 [tokens]) of cos and sin (int32 [rows, rot / 2] at 2^frac; all three None: no rotation), queries times q_mul / 2^frac;
     returns (q_out0, q_out1, opened_bits), the outputs None without queries."""
     import torch
-    pointer = _cache_arg(cache)
+    if stream is None and type(cache) is Cache:
+        done = _native.append(cache.struct, k0, k1, v0, v1, slots, positions, cos, sin, frac, seed, q0, q1, q_mul, q_out0, q_out1)
+        if done is not NotImplemented:
+            return done
+    cache = _cache_arg(cache)
     tokens = slots.shape[0] if isinstance(slots, torch.Tensor) and slots.dim() else 0
     kv = [_typed(t, torch.int64, tokens, cache.heads, cache.dim) for t in (k0, k1, v0, v1)]
     rows, half, turn = 0, 0, [None, None, None]
@@ -675,18 +697,18 @@ def hb_cache_append(cache, k0, k1, v0, v1, slots, positions, cos, sin, frac, see
     if q0 is not None or q1 is not None:
         heads = q0.shape[1] if isinstance(q0, torch.Tensor) and q0.dim() == 3 else None
         if q_out0 is None:
-            q_out0 = torch.empty_like(q0)
+            q_out0 = _made_for(stream, lambda: torch.empty_like(q0))
         if q_out1 is None:
-            q_out1 = torch.empty_like(q1)
+            q_out1 = _made_for(stream, lambda: torch.empty_like(q1))
         q = [_typed(t, torch.int64, tokens, heads, cache.dim) for t in (q0, q1, q_out0, q_out1)]
     bits = ctypes.c_uint64(0)
-    _check(load().hb_cache_append(pointer, *kv, tokens, _typed(slots, torch.int64, tokens), *turn, rows, 2 * half, int(frac), q[0], q[1], heads,
+    _check(load().hb_cache_append(ctypes.byref(cache), *kv, tokens, _typed(slots, torch.int64, tokens), *turn, rows, 2 * half, int(frac), q[0], q[1], heads,
                                   int(q_mul), int(seed) & (2**64 - 1), q[2], q[3], ctypes.byref(bits), _stream_handle(stream)))
     return q_out0, q_out1, int(bits.value)
 
 
 def hb_attention_workspace_bytes(cache, batch, q_heads, max_len):
-    return int(load().hb_attention_workspace_bytes(_cache_arg(cache), int(batch), int(q_heads), int(max_len)))
+    return int(load().hb_attention_workspace_bytes(ctypes.byref(_cache_arg(cache)), int(batch), int(q_heads), int(max_len)))
 
 
 def hb_attention(cache, q0, q1, page_table, lens, max_len, k, m, seed, out0=None, out1=None, workspace=None, stream=None):
@@ -694,18 +716,22 @@ def hb_attention(cache, q0, q1, page_table, lens, max_len, k, m, seed, out0=None
     [batch]), with ReLU on the slice [k, m) of the scores; returns (out0, out1, opened_bits).  workspace: a uint8 CUDA tensor, allocated here
     unless one is passed."""
     import torch
-    pointer = _cache_arg(cache)
+    if stream is None and type(cache) is Cache:
+        done = _native.attention(cache.struct, q0, q1, page_table, lens, max_len, k, m, seed, out0, out1, workspace)
+        if done is not NotImplemented:
+            return done
+    pointer = ctypes.byref(_cache_arg(cache))
     if out0 is None:
-        out0 = torch.empty_like(q0)
+        out0 = _made_for(stream, lambda: torch.empty_like(q0))
     if out1 is None:
-        out1 = torch.empty_like(q1)
-    at = [_typed(q0, torch.int64, None, None, cache.dim)]
-    batch, heads = q0.shape[:2]
-    at += [_typed(t, torch.int64, batch, heads, cache.dim) for t in (q1, out0, out1)]
+        out1 = _made_for(stream, lambda: torch.empty_like(q1))
+    at = [_typed(q0, torch.int64, None, None, cache.keys.shape[3])]
+    batch, heads, dim = q0.shape
+    at += [_typed(t, torch.int64, batch, heads, dim) for t in (q1, out0, out1)]
     at += [_typed(page_table, torch.int32, batch, None), _typed(lens, torch.int32, batch)]
     if workspace is None:
         need = int(load().hb_attention_workspace_bytes(pointer, batch, heads, int(max_len)))
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q0.device)
+        workspace = _made_for(stream, lambda: torch.empty(max(need, 256), dtype=torch.uint8, device=q0.device))
     room = _typed(workspace, torch.uint8, None)
     bits = ctypes.c_uint64(0)
     _check(load().hb_attention(pointer, at[0], at[1], batch, heads, at[4], page_table.shape[1], at[5], int(max_len), int(k), int(m),
