@@ -3,6 +3,8 @@
 #include "hb_check.hpp"
 #include "hb_launch.hpp"
 
+#include <type_traits>
+
 namespace {
 
 // What a cache has to be, whatever is done with it.
@@ -37,7 +39,7 @@ size_t round_up(size_t n) { return (n + 255) & ~(size_t)255; }
 // Workspace of hb_attention: shares of the scores, then the splits' partial sums.
 struct AttentionLayout {
     size_t scores1, parts, bytes;
-    uint32_t splits, per_split;
+    uint32_t splits, per_split, per_scores;
 };
 
 bool attention_sizes(const hb_cache *cache, size_t batch, int q_heads, size_t max_len)
@@ -46,20 +48,73 @@ bool attention_sizes(const hb_cache *cache, size_t batch, int q_heads, size_t ma
            max_len <= ((size_t)1 << 30) && batch * q_heads * max_len <= HB_MAX_ELEMENTS;
 }
 
+// Query heads that a workgroup takes together, a power of two up to eight, and how many such chunks a head of the cache has.
+int heads_together(const hb_cache *cache, int q_heads)
+{
+    const int group = q_heads / cache->heads, chunks = (group + 7) / 8, each = (group + chunks - 1) / chunks;
+    return each <= 1 ? 1 : each <= 2 ? 2 : each <= 4 ? 4 : 8;
+}
+size_t head_chunks(const hb_cache *cache, int q_heads)
+{
+    const int group = q_heads / cache->heads, together = heads_together(cache, q_heads);
+    return (size_t)((group + together - 1) / together);
+}
+
 AttentionLayout attention_layout(const hb_cache *cache, size_t batch, int q_heads, size_t max_len)
 {
     AttentionLayout lay = {};
     const size_t scores = round_up(8 * batch * q_heads * max_len), numbers = batch * q_heads * cache->dim;
-    lay.per_split = 256;
+    // Positions of a workgroup: as many as leave the chip about four workgroups for each compute unit.
+    const size_t groups = batch * cache->heads * head_chunks(cache, q_heads);
+    size_t per = 1024;
+    while (per > 64 && groups * ((max_len + per - 1) / per) < 1024) per /= 2;
+    lay.per_scores = (uint32_t)per;
+    lay.per_split = (uint32_t)(per < hb::kValueChunk ? hb::kValueChunk : per);
     lay.splits = (uint32_t)((max_len + lay.per_split - 1) / lay.per_split);
-    while (lay.splits > 64) {
-        lay.per_split *= 2;
-        lay.splits = (uint32_t)((max_len + lay.per_split - 1) / lay.per_split);
-    }
     lay.scores1 = scores;
     lay.parts = 2 * scores;
     lay.bytes = 2 * scores + round_up(16 * numbers * lay.splits);
     return lay;
+}
+
+// body(std::integral_constant<int, GT>) for the number of query heads a workgroup takes.
+template <class Body>
+void with_heads(int together, const Body &body)
+{
+    switch (together) {
+    case 1: return body(std::integral_constant<int, 1>{});
+    case 2: return body(std::integral_constant<int, 2>{});
+    case 4: return body(std::integral_constant<int, 4>{});
+    default: return body(std::integral_constant<int, 8>{});
+    }
+}
+
+void launch_scores(const hb::AttentionArgs &a, int together, dim3 grid, hipStream_t stream)
+{
+    with_heads(together, [&](auto heads) {
+        constexpr int GT = decltype(heads)::value;
+        const dim3 block(hb::kAttentionBlock);
+        switch ((a.cache.dim + 63) / 64) {
+        case 1: hipLaunchKernelGGL((hb::attention_scores_kernel<GT, 1>), grid, block, 0, stream, a); break;
+        case 2: hipLaunchKernelGGL((hb::attention_scores_kernel<GT, 2>), grid, block, 0, stream, a); break;
+        case 3: hipLaunchKernelGGL((hb::attention_scores_kernel<GT, 3>), grid, block, 0, stream, a); break;
+        default: hipLaunchKernelGGL((hb::attention_scores_kernel<GT, 4>), grid, block, 0, stream, a); break;
+        }
+    });
+}
+
+void launch_values(const hb::AttentionArgs &a, int together, dim3 grid, hipStream_t stream)
+{
+    with_heads(together, [&](auto heads) {
+        constexpr int GT = decltype(heads)::value;
+        const dim3 block(hb::kAttentionBlock);
+        switch ((a.cache.dim + 63) / 64) {
+        case 1: hipLaunchKernelGGL((hb::attention_values_kernel<GT, 1>), grid, block, 0, stream, a); break;
+        case 2: hipLaunchKernelGGL((hb::attention_values_kernel<GT, 2>), grid, block, 0, stream, a); break;
+        case 3: hipLaunchKernelGGL((hb::attention_values_kernel<GT, 3>), grid, block, 0, stream, a); break;
+        default: hipLaunchKernelGGL((hb::attention_values_kernel<GT, 4>), grid, block, 0, stream, a); break;
+        }
+    });
 }
 
 }  // namespace
@@ -168,30 +223,30 @@ int hb_attention(const hb_cache *cache, const int64_t *q0, const int64_t *q1, si
         a.batch = (uint32_t)batch;
         a.q_heads = (uint32_t)q_heads;
         a.max_len = (uint32_t)max_len;
-        a.splits = lay.splits;
+        a.per_scores = lay.per_scores;
         a.per_split = lay.per_split;
         const hb::GroupLauncher relu = hb::launcher_table().f[hb::kRelu][m - k - 1];
         if (relu == nullptr) return hb::fail_hip(hipErrorInvalidDeviceFunction, "no kernel was built for this slice width");
         hipError_t e = hipSuccess;
-        const dim3 block(hb::kAttentionBlock);
         if (max_len != 0) {
-            const uint64_t blocks = (scores + hb::kAttentionBlock / 64 - 1) / (hb::kAttentionBlock / 64);
-            if (blocks > 0x7fffffffull) return HB_EINVAL;
-            hipLaunchKernelGGL(hb::attention_scores_kernel, dim3((unsigned)blocks), block, 0, (hipStream_t)stream, a);
+            const int together = heads_together(cache, q_heads);
+            const uint64_t groups = batch * cache->heads * head_chunks(cache, q_heads);
+            const uint64_t pieces = (max_len + lay.per_scores - 1) / lay.per_scores;
+            if (groups > 0x7fffffffull || pieces > 65535) return HB_EINVAL;
+            launch_scores(a, together, dim3((unsigned)groups, (unsigned)pieces), (hipStream_t)stream);
             e = hipGetLastError();
             if (e == hipSuccess) {
                 e = relu(a.scores[0], a.scores[1], scores, k, hb::stream_word(seed_relu, 0), hb::stream_word(seed_relu, 1), a.scores[0], a.scores[1],
                          (hipStream_t)stream);
             }
             if (e == hipSuccess) {
-                const uint64_t over = ((uint64_t)batch * q_heads * cache->dim + hb::kAttentionBlock - 1) / hb::kAttentionBlock;
-                hipLaunchKernelGGL(hb::attention_values_kernel, dim3((unsigned)over, lay.splits), block, 0, (hipStream_t)stream, a);
+                launch_values(a, together, dim3((unsigned)groups, lay.splits), (hipStream_t)stream);
                 e = hipGetLastError();
             }
         }
         if (e == hipSuccess) {
             const unsigned over = (unsigned)(((uint64_t)q_heads * cache->dim + hb::kAttentionBlock - 1) / hb::kAttentionBlock);
-            hipLaunchKernelGGL(hb::attention_join_kernel, dim3(over, (unsigned)batch), block, 0, (hipStream_t)stream, a);
+            hipLaunchKernelGGL(hb::attention_join_kernel, dim3(over, (unsigned)batch), dim3(hb::kAttentionBlock), 0, (hipStream_t)stream, a);
             e = hipGetLastError();
         }
         if (e != hipSuccess) return hb::fail_hip(e, "kernel launch");

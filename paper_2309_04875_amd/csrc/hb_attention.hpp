@@ -2,6 +2,8 @@
 #pragma once
 
 #include "hb_cache.hpp"
+#include "hb_digits.hpp"
+#include "hb_kernels.hpp"
 
 namespace hb {
 
@@ -10,11 +12,11 @@ struct AttentionArgs {
     const uint64_t *q[2];                 // [batch][q_heads][dim]
     uint64_t *out[2];
     uint64_t *scores[2];                  // [batch][q_heads][max_len], workspace
-    uint64_t *parts;                      // [splits][batch][q_heads][dim][2], workspace
+    uint64_t *parts;                      // [splits][2][batch][q_heads][dim], workspace
     const int32_t *table, *lens;          // [batch][table_width], [batch]
     uint64_t table_width;
     uint64_t seed_q, seed_s, seed_p, seed_o;
-    uint32_t batch, q_heads, max_len, splits, per_split;
+    uint32_t batch, q_heads, max_len, per_scores, per_split;    // positions of a workgroup
 };
 
 __device__ __forceinline__ uint32_t length_of(const AttentionArgs &a, uint32_t b)
@@ -23,71 +25,337 @@ __device__ __forceinline__ uint32_t length_of(const AttentionArgs &a, uint32_t b
     return n < 0 ? 0 : ((uint32_t)n > a.max_len ? a.max_len : (uint32_t)n);
 }
 
-constexpr int kAttentionBlock = 256;
+constexpr int kAttentionBlock = 256, kAttentionWaves = kAttentionBlock / 64;
 
-// Scores: one wavefront per (sequence, query head, position), lanes over the dimensions.
-__global__ void __launch_bounds__(kAttentionBlock)
-attention_scores_kernel(AttentionArgs a)
+// Both products of attention are sums of Beaver products of few fresh vectors with many masked numbers D = x - b of the cache.  With a = a_0 + a_1 and
+// eps = (q or p) - a the two parties' sums are, their terms collected by what is read from the cache or drawn for it,
+//   party 0:  sum eps (b_0 + D) + D a_0              = sum b_0 eps + D (eps + a_0)
+//   party 1:  sum eps b_1 + D a_1 + (b_0 + b_1) a    = sum b_0 a   + b_1 (a + eps) + D a_1      (the last term: the dealer's triple)
+// so three matrices, b_0, b_1 and D, meet two vectors for each query head, one for each party: b_0 {eps, a}, b_1 {0, a + eps}, D {eps + a_0, a_1}.
+//
+// In digits: sum over s of 2^(8s) of sum over i <= s of (digit i of the matrix) (digit s - i of the vectors).  Matrices are the left operands, 16
+// rows a tile; the right operand of matrix digit i has a column (s, v) for every weight 2^(8s) and vector v = party * GT + head that holds digit s - i
+// of v, nothing where s < i: 16 GT columns, GT tiles.  The vectors' digits lie in LDS as planes [digit][v], the columns of digit i
+// are the planes 2 GT i further up, and planes of zeros lie before the first; a tile whose columns all have s < i is left out (36 of 64
+// products at GT = 8, 20 of 32 at GT = 4).  int32 sums hold 2^17 a place: 2^14 places at most go into one.
+constexpr int kZeroPlanes = 16, kMostPlaces = 1 << 14;
+
+template <int GT>
+struct Vectors {
+    static constexpr int nv = 2 * GT, planes = kZeroPlanes + 8 * nv;          // planes of one matrix
+    static constexpr bool used(int i, int tile) { return i * nv <= 16 * tile + 15; }
+};
+
+// Digits of four consecutive places of vector v, at byte `at` of its planes.
+template <int GT>
+__device__ __forceinline__ void store_vector(uint8_t *planes, uint32_t stride, uint32_t v, uint32_t at, const uint64_t (&x)[4])
 {
-    const CacheView &c = a.cache;
-    const uint64_t j = (uint64_t)blockIdx.x * (kAttentionBlock / 64) + threadIdx.x / 64;
-    if (j >= (uint64_t)a.batch * a.q_heads * a.max_len) return;
-    const uint32_t lane = threadIdx.x % 64, t = (uint32_t)(j % a.max_len);
-    const uint64_t row = j / a.max_len;
-    const uint32_t b = (uint32_t)(row / a.q_heads), head = (uint32_t)(row % a.q_heads) / (a.q_heads / c.heads);
-    const int64_t page = t < length_of(a, b) ? a.table[b * a.table_width + t / c.page] : -1;
-    Pair s{0, 0};
-    if (page >= 0 && page < c.pages) {
-        const uint64_t masks = stream_word(c.page_seeds[page], 0);
-        const uint64_t *keys = c.keys + page * page_numbers(c);
-        uint64_t c1 = 0;
-        for (uint32_t d = lane; d < c.dim; d += 64) {
-            const uint64_t i = row * c.dim + d, e = place_in_page(c, head, t % c.page, d);
-            const uint64_t a0 = stream_word(a.seed_q, 2 * i), a1 = stream_word(a.seed_q, 2 * i + 1);
-            const uint64_t eps = (a.q[0][i] - a0) + (a.q[1][i] - a1);                              // opened
-            const uint64_t b0 = stream_word(masks, 2 * e), b1 = stream_word(masks, 2 * e + 1), del = keys[e];
-            s.p0 += eps * (b0 + del) + del * a0;
-            s.p1 += eps * b1 + del * a1;
-            c1 += (a0 + a1) * (b0 + b1);                                                         // the dealer's triple
-        }
-        const uint64_t z = state_of(a.seed_s, 5 * j), c0 = mix64(z);
-        s.p0 = wave_sum(s.p0) + c0;
-        s.p1 = wave_sum(s.p1 + c1) - c0;
-        s = truncate_drawn(s, 16, z + kGamma);
-    }
-    if (lane == 0) {
-        a.scores[0][j] = s.p0;
-        a.scores[1][j] = s.p1;
+    uint32_t d[8];
+    digits_of(x, d);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) *reinterpret_cast<uint32_t *>(planes + (kZeroPlanes + j * Vectors<GT>::nv + v) * stride + at) = d[j];
+}
+
+// The vectors of one query head for the three matrices.
+template <int GT>
+__device__ __forceinline__ void store_vectors(uint8_t *lds, uint32_t stride, uint32_t head, uint32_t at, const uint64_t (&eps)[4], const uint64_t (&a0)[4],
+                                              const uint64_t (&a1)[4])
+{
+    const uint32_t matrix = Vectors<GT>::planes * stride;
+    uint64_t v[4];
+    store_vector<GT>(lds, stride, head, at, eps);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = a0[j] + a1[j];
+    store_vector<GT>(lds, stride, GT + head, at, v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] += eps[j];
+    store_vector<GT>(lds + matrix, stride, GT + head, at, v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = eps[j] + a0[j];
+    store_vector<GT>(lds + 2 * matrix, stride, head, at, v);
+    store_vector<GT>(lds + 2 * matrix, stride, GT + head, at, a1);
+}
+
+// Zeros where no vector is: before the planes, and party 0's vectors for b_1.
+template <int GT>
+__device__ __forceinline__ void clear_planes(uint8_t *lds, uint32_t stride)
+{
+    const uint32_t matrix = Vectors<GT>::planes * stride, words = stride / 4;
+    for (uint32_t i = threadIdx.x; i < 3 * kZeroPlanes * words; i += kAttentionBlock)
+        *reinterpret_cast<uint32_t *>(lds + i / (kZeroPlanes * words) * matrix + i % (kZeroPlanes * words) * 4) = 0;
+    for (uint32_t i = threadIdx.x; i < 8 * GT * words; i += kAttentionBlock) {
+        const uint32_t plane = i / words;
+        *reinterpret_cast<uint32_t *>(lds + matrix + (kZeroPlanes + plane / GT * Vectors<GT>::nv + plane % GT) * stride + i % words * 4) = 0;
     }
 }
 
-// The product with the values: one thread per (split, sequence, query head, dimension).
+typedef uint32_t MatrixDigits[8][4];      // a lane's 16 numbers of a row: digit, four numbers a word
+
+// sums += digits times one matrix's vectors; column: this lane's first plane (lane mod 16) at its places.
+template <int GT>
+__device__ __forceinline__ void multiply(i32x4_t (&sums)[GT], const MatrixDigits &d, const uint8_t *column, uint32_t stride)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const i32x4_t left{(int)d[i][0], (int)d[i][1], (int)d[i][2], (int)d[i][3]};
+#pragma unroll
+        for (int tile = 0; tile < GT; ++tile) {
+            if (!Vectors<GT>::used(i, tile)) continue;
+            const i32x4_t right = *reinterpret_cast<const i32x4_t *>(column + (kZeroPlanes + 16 * tile - i * Vectors<GT>::nv) * stride);
+            sums[tile] = mfma_16x16x64(left, right, sums[tile]);
+        }
+    }
+}
+
+__device__ __forceinline__ void digits_at(MatrixDigits &d, int s, const uint64_t (&v)[4])
+{
+    uint32_t w[8];
+    digits_of(v, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) d[i][s] = w[i];
+}
+
+// The weights 2^(8s) put together: value[r] of vector v = lane mod 2 GT and row 4 (lane / 16) + r, in all lanes with that v.
+template <int GT>
+__device__ __forceinline__ void join_digits(const i32x4_t (&sums)[GT], uint32_t lane, uint64_t (&value)[4])
+{
+    constexpr int kPer = 16 / Vectors<GT>::nv;                 // values of s in a tile
+    // 2^(8 s') of this lane's s' = s mod kPer
+    uint64_t weight = 1;
+#pragma unroll
+    for (int s = 1; s < kPer; ++s) weight = lane % 16 / Vectors<GT>::nv == s ? 1ull << (8 * s) : weight;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        uint64_t y = 0;
+#pragma unroll
+        for (int tile = 0; tile < GT; ++tile) y += (uint64_t)(int64_t)sums[tile][r] << (8 * kPer * tile);
+        if constexpr (kPer > 1) y *= weight;
+#pragma unroll
+        for (int step = Vectors<GT>::nv; step < 16; step *= 2) y += __shfl_xor((unsigned long long)y, step, 64);
+        value[r] = y;
+    }
+}
+
+// Where a position of a sequence lies: its page, or -1 for one behind the end and for a hole.
+__device__ __forceinline__ int64_t page_of(const AttentionArgs &a, uint32_t b, uint32_t t, uint32_t length)
+{
+    if (t >= length) return -1;
+    const int64_t page = a.table[b * a.table_width + t / a.cache.page];
+    return page < (int64_t)a.cache.pages ? page : -1;
+}
+
+// What a workgroup works on: a sequence, a head of the cache and up to GT of its query heads.
+struct HeadChunk {
+    uint32_t b, head, first, count;       // query heads first .. first + count - 1
+};
+template <int GT>
+__device__ __forceinline__ HeadChunk head_chunk(const AttentionArgs &a, uint32_t index)
+{
+    const uint32_t group = a.q_heads / a.cache.heads, chunks = (group + GT - 1) / GT;
+    const uint32_t chunk = index % chunks, head = index / chunks % a.cache.heads, b = index / chunks / a.cache.heads;
+    const uint32_t left = group - chunk * GT;
+    return HeadChunk{b, head, head * group + chunk * GT, left < GT ? left : GT};
+}
+
+// Scores.  A wavefront takes 16 positions at a time: a row of its tile is a key, lane l has row l mod 16 and of every 64 dimensions the pairs
+// 8 j + 2 (l / 16), j = 0 .. 7 (the lanes of a row read 64 bytes side by side).
+template <int GT, int ND>
+__global__ void __launch_bounds__(kAttentionBlock)
+attention_scores_kernel(AttentionArgs a)
+{
+    constexpr uint32_t kStride = 64 * ND + 16;
+    __shared__ __align__(16) uint8_t lds[3 * Vectors<GT>::planes * kStride];
+    const CacheView &c = a.cache;
+    const HeadChunk h = head_chunk<GT>(a, blockIdx.x);
+    const uint32_t first = blockIdx.y * a.per_scores, length = __builtin_amdgcn_readfirstlane(length_of(a, h.b));
+    const uint32_t end = first + a.per_scores < a.max_len ? first + a.per_scores : a.max_len;
+    const uint64_t row0 = (uint64_t)h.b * a.q_heads + h.first;
+    if (first >= length) {                                    // all of it behind the sequence's end
+        const uint32_t count = end - first;
+        for (uint32_t i = threadIdx.x; i < h.count * count; i += kAttentionBlock) {
+            const uint64_t j = (row0 + i / count) * a.max_len + first + i % count;
+            a.scores[0][j] = 0;
+            a.scores[1][j] = 0;
+        }
+        return;
+    }
+    clear_planes<GT>(lds, kStride);
+    for (uint32_t i = threadIdx.x; i < GT * ND * 16; i += kAttentionBlock) {
+        const uint32_t head = i / (ND * 16), piece = i / 4 % (4 * ND), g = i % 4;          // four dimensions: pairs of two j
+        const uint32_t d0 = 16 * piece + 2 * g;
+        uint64_t eps[4], a0[4], a1[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t d = d0 + 8 * (j / 2) + j % 2;
+            const bool there = head < h.count && d < c.dim;
+            const uint64_t at = (row0 + head) * c.dim + d;
+            const uint64_t z = state_of(a.seed_q, 2 * at);
+            a0[j] = there ? mix64(z) : 0;
+            a1[j] = there ? mix64(z + kGamma) : 0;
+            eps[j] = there ? (a.q[0][at] - a0[j]) + (a.q[1][at] - a1[j]) : 0;              // opened
+        }
+        store_vectors<GT>(lds, kStride, head, piece / 4 * 64 + 16 * g + piece % 4 * 4, eps, a0, a1);
+    }
+    __syncthreads();
+    const uint32_t lane = threadIdx.x % 64, g = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint8_t *column = lds + (lane % 16) * kStride + 16 * g;
+    constexpr uint32_t kMatrix = Vectors<GT>::planes * kStride;
+    for (uint32_t t0 = first + 16 * wave; t0 < end; t0 += 16 * kAttentionWaves) {
+        const uint32_t t = t0 + lane % 16;
+        const int64_t page = page_of(a, h.b, t, length);
+        const bool there = page >= 0;
+        const uint64_t place = place_in_page(c, h.head, t % c.page, 2 * g);
+        const uint64_t *keys = c.keys + (there ? page * page_numbers(c) + place : 0);
+        const uint64_t z0 = state_of(there ? stream_word(c.page_seeds[page], 0) : 0, 2 * place);
+        i32x4_t sums[GT] = {};
+#pragma unroll
+        for (int chunk = 0; chunk < ND; ++chunk) {
+            uint64_t delta[16];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                U64x2 v{0, 0};
+                if (there && 64 * chunk + 8 * j + 2 * g < c.dim) v = load_stream2(keys + 64 * chunk + 8 * j);
+                delta[2 * j] = v.a;
+                delta[2 * j + 1] = v.b;
+            }
+            MatrixDigits d;
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    uint64_t b[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) b[j] = mix64(z0 + (uint64_t)(2 * (64 * chunk + 8 * (2 * s + j / 2) + j % 2) + p) * kGamma);
+                    digits_at(d, s, b);
+                }
+                multiply<GT>(sums, d, column + p * kMatrix + 64 * chunk, kStride);
+            }
+#pragma unroll
+            for (int s = 0; s < 4; ++s) digits_at(d, s, {delta[4 * s], delta[4 * s + 1], delta[4 * s + 2], delta[4 * s + 3]});
+            multiply<GT>(sums, d, column + 2 * kMatrix + 64 * chunk, kStride);
+        }
+        uint64_t mine[4], other[4];
+        join_digits<GT>(sums, lane, mine);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) other[r] = __shfl_xor((unsigned long long)mine[r], GT, 64);
+        // The lanes of a head share out its four rows.
+        const bool party1 = (lane & GT) != 0;
+        const uint32_t head = lane % GT, part = lane % 16 / GT;
+        constexpr int kRows = GT == 8 ? 2 : 1;
+        if (part * kRows < 4 && head < h.count) {
+#pragma unroll
+            for (int x = 0; x < kRows; ++x) {
+                Pair y{mine[x], other[x]};
+#pragma unroll
+                for (int r = 1; r < 4; ++r) {
+                    if (part * kRows + x == r) y = Pair{mine[r], other[r]};
+                }
+                if (party1) y = Pair{y.p1, y.p0};
+                const uint32_t at = t0 + 4 * g + part * kRows + x;
+                if (at >= end) continue;
+                const uint64_t j = (row0 + head) * a.max_len + at;
+                Pair score{0, 0};
+                if (page_of(a, h.b, at, length) >= 0) {
+                    const uint64_t z = state_of(a.seed_s, 5 * j), c0 = mix64(z);
+                    score = truncate_drawn(Pair{y.p0 + c0, y.p1 - c0}, 16, z + kGamma);
+                }
+                a.scores[0][j] = score.p0;
+                a.scores[1][j] = score.p1;
+            }
+        }
+    }
+}
+
+// The product with the values.  A row of a wavefront's tile is a dimension (DT tiles of 16), lane l takes 16 of every 64 positions; the workgroup makes
+// the weights' vectors of 128 positions at a time.
+constexpr int kValueChunk = 128;
+
+template <int GT, int DT>
 __global__ void __launch_bounds__(kAttentionBlock)
 attention_values_kernel(AttentionArgs a)
 {
+    constexpr uint32_t kStride = kValueChunk + 16;
+    __shared__ __align__(16) uint8_t lds[3 * Vectors<GT>::planes * kStride];
+    __shared__ uint64_t row_at[kValueChunk], row_state[kValueChunk];       // a position's numbers and masks
     const CacheView &c = a.cache;
-    const uint64_t i = (uint64_t)blockIdx.x * kAttentionBlock + threadIdx.x;
-    const uint64_t rows = (uint64_t)a.batch * a.q_heads, numbers = rows * c.dim;
-    if (i >= numbers) return;
-    const uint32_t d = (uint32_t)(i % c.dim);
-    const uint64_t row = i / c.dim;
-    const uint32_t b = (uint32_t)(row / a.q_heads), head = (uint32_t)(row % a.q_heads) / (a.q_heads / c.heads);
-    const uint32_t length = length_of(a, b), first = blockIdx.y * a.per_split;
-    const uint32_t last = first + a.per_split < length ? first + a.per_split : length;
-    Pair o{0, 0};
-    for (uint32_t t = first; t < last; ++t) {
-        const int64_t page = a.table[b * a.table_width + t / c.page];
-        if (page < 0 || page >= c.pages) continue;
-        const uint64_t masks = stream_word(c.page_seeds[page], 1), j = row * a.max_len + t, e = place_in_page(c, head, t % c.page, d);
-        const uint64_t a0 = stream_word(a.seed_p, 2 * j), a1 = stream_word(a.seed_p, 2 * j + 1);
-        const uint64_t eps = (a.scores[0][j] - a0) + (a.scores[1][j] - a1);                          // opened
-        const uint64_t b0 = stream_word(masks, 2 * e), b1 = stream_word(masks, 2 * e + 1), del = c.values[page * page_numbers(c) + e];
-        o.p0 += eps * (b0 + del) + del * a0;
-        o.p1 += eps * b1 + del * a1 + (a0 + a1) * (b0 + b1);
+    const HeadChunk h = head_chunk<GT>(a, blockIdx.x);
+    const uint32_t length = __builtin_amdgcn_readfirstlane(length_of(a, h.b));
+    const uint32_t first = blockIdx.y * a.per_split, end = first + a.per_split < length ? first + a.per_split : length;
+    if (first >= length) return;                              // the join does not read it
+    const uint64_t row0 = (uint64_t)h.b * a.q_heads + h.first;
+    const uint32_t lane = threadIdx.x % 64, g = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint8_t *column = lds + (lane % 16) * kStride + 16 * g;
+    constexpr uint32_t kMatrix = Vectors<GT>::planes * kStride;
+    clear_planes<GT>(lds, kStride);
+    i32x4_t sums[DT][GT] = {};
+    for (uint32_t t0 = first; t0 < end; t0 += kValueChunk) {
+        for (uint32_t i = threadIdx.x; i < kValueChunk; i += kAttentionBlock) {
+            const int64_t page = page_of(a, h.b, t0 + i, end);
+            const uint64_t place = place_in_page(c, h.head, (t0 + i) % c.page, 0);
+            row_at[i] = page >= 0 ? page * page_numbers(c) + place : ~0ull;
+            row_state[i] = page >= 0 ? state_of(stream_word(c.page_seeds[page], 1), 2 * place) : 0;
+        }
+        for (uint32_t i = threadIdx.x; i < GT * kValueChunk / 4; i += kAttentionBlock) {
+            const uint32_t head = i / (kValueChunk / 4), at = i % (kValueChunk / 4) * 4;
+            uint64_t eps[4], a0[4], a1[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t t = t0 + at + j;
+                const bool there = head < h.count && page_of(a, h.b, t, end) >= 0;
+                const uint64_t n = (row0 + head) * a.max_len + t, z = state_of(a.seed_p, 2 * n);
+                a0[j] = there ? mix64(z) : 0;
+                a1[j] = there ? mix64(z + kGamma) : 0;
+                eps[j] = there ? (a.scores[0][n] - a0[j]) + (a.scores[1][n] - a1[j]) : 0;  // opened
+            }
+            store_vectors<GT>(lds, kStride, head, at, eps, a0, a1);
+        }
+        __syncthreads();
+        for (uint32_t block = 0; block < kValueChunk / 64 && t0 + 64 * block < end; ++block) {
+#pragma unroll
+            for (int tile = 0; tile < DT; ++tile) {
+                const uint32_t dim = 16 * (wave * DT + tile) + lane % 16;
+                if (16 * (wave * DT + tile) >= c.dim) continue;
+                uint64_t delta[16], z[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const uint64_t at = row_at[64 * block + 16 * g + j];
+                    z[j] = row_state[64 * block + 16 * g + j] + (uint64_t)(2 * dim) * kGamma;
+                    delta[j] = at != ~0ull && dim < c.dim ? load_stream(c.values + at + dim) : 0;
+                }
+                MatrixDigits d;
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) {
+                        uint64_t b[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) b[j] = mix64(z[4 * s + j] + (uint64_t)p * kGamma);
+                        digits_at(d, s, b);
+                    }
+                    multiply<GT>(sums[tile], d, column + p * kMatrix + 64 * block, kStride);
+                }
+#pragma unroll
+                for (int s = 0; s < 4; ++s) digits_at(d, s, {delta[4 * s], delta[4 * s + 1], delta[4 * s + 2], delta[4 * s + 3]});
+                multiply<GT>(sums[tile], d, column + 2 * kMatrix + 64 * block, kStride);
+            }
+        }
+        __syncthreads();
     }
-    uint64_t *to = a.parts + 2 * (blockIdx.y * numbers + i);
-    to[0] = o.p0;
-    to[1] = o.p1;
+    // One partial sum for each number of the output and party, in lanes of the first half of a tile's columns that hold it.
+    const uint64_t numbers = (uint64_t)a.batch * a.q_heads * c.dim;
+    const uint32_t head = lane % GT;
+    const uint64_t party = (lane & GT) != 0;
+#pragma unroll
+    for (int tile = 0; tile < DT; ++tile) {
+        uint64_t y[4];
+        join_digits<GT>(sums[tile], lane, y);
+        if (lane % 16 >= Vectors<GT>::nv || head >= h.count) continue;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const uint32_t dim = 16 * (wave * DT + tile) + 4 * g + r;
+            if (dim < c.dim) a.parts[(2 * (uint64_t)blockIdx.y + party) * numbers + (row0 + head) * c.dim + dim] = y[r];
+        }
+    }
 }
 
 // Joins the splits and divides by the length: a truncation by its whole bits, a factor in (1/2, 1] for the rest.
@@ -103,9 +371,10 @@ attention_join_kernel(AttentionArgs a)
     if (length != 0) {
         const uint64_t z = state_of(a.seed_o, 9 * i), c0 = mix64(z);
         o = Pair{c0, 0 - c0};
-        for (uint32_t s = 0; s < a.splits; ++s) {
-            o.p0 += a.parts[2 * (s * numbers + i)];
-            o.p1 += a.parts[2 * (s * numbers + i) + 1];
+        const uint32_t splits = (length + a.per_split - 1) / a.per_split;
+        for (uint32_t s = 0; s < splits; ++s) {
+            o.p0 += a.parts[2 * (uint64_t)s * numbers + i];
+            o.p1 += a.parts[(2 * (uint64_t)s + 1) * numbers + i];
         }
         const int whole = 31 - __builtin_clz(length);
         const uint64_t factor = ((1ull << (16 + whole)) + length / 2) / length;
