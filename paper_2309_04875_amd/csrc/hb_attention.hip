@@ -45,7 +45,7 @@ struct AttentionLayout {
 bool attention_sizes(const hb_cache *cache, size_t batch, int q_heads, size_t max_len)
 {
     return check_cache(cache) == HB_OK && q_heads >= cache->heads && q_heads <= 65536 && q_heads % cache->heads == 0 && batch <= 65535 &&
-           max_len <= ((size_t)1 << 30) && batch * q_heads * max_len <= HB_MAX_ELEMENTS;
+           max_len <= ((size_t)1 << 29) && batch * q_heads * max_len <= HB_MAX_ELEMENTS;
 }
 
 // Query heads that a workgroup takes together, a power of two up to eight, and how many such chunks a head of the cache has.
@@ -64,12 +64,13 @@ AttentionLayout attention_layout(const hb_cache *cache, size_t batch, int q_head
 {
     AttentionLayout lay = {};
     const size_t scores = round_up(8 * batch * q_heads * max_len), numbers = batch * q_heads * cache->dim;
-    // Positions of a workgroup: as many as leave the chip about four workgroups for each compute unit.
-    const size_t groups = batch * cache->heads * head_chunks(cache, q_heads);
-    size_t per = 1024;
-    while (per > 64 && groups * ((max_len + per - 1) / per) < 1024) per /= 2;
+    // Positions of a workgroup, a multiple of 128: what gives every compute unit two workgroups at a time, four where lengths may differ.
+    const size_t some = batch != 0 ? batch : 1, groups = some * cache->heads * head_chunks(cache, q_heads), pieces = ((batch > 1 ? 1024 : 512) + groups - 1) / groups;
+    size_t per = ((max_len + pieces - 1) / pieces + 127) / 128 * 128;
+    if (per > hb::kMostPlaces) per = hb::kMostPlaces;
+    if (per < 128) per = 128;
     lay.per_scores = (uint32_t)per;
-    lay.per_split = (uint32_t)(per < hb::kValueChunk ? hb::kValueChunk : per);
+    lay.per_split = (uint32_t)per;
     lay.splits = (uint32_t)((max_len + lay.per_split - 1) / lay.per_split);
     lay.scores1 = scores;
     lay.parts = 2 * scores;
@@ -105,15 +106,12 @@ void launch_scores(const hb::AttentionArgs &a, int together, dim3 grid, hipStrea
 
 void launch_values(const hb::AttentionArgs &a, int together, dim3 grid, hipStream_t stream)
 {
+    const unsigned tiles = (a.cache.dim + 15) / 16, most = hb::kAttentionWaves;
+    grid.z = (tiles + most - 1) / most;
+    const dim3 block(64 * (grid.z > 1 ? most : tiles));
     with_heads(together, [&](auto heads) {
         constexpr int GT = decltype(heads)::value;
-        const dim3 block(hb::kAttentionBlock);
-        switch ((a.cache.dim + 63) / 64) {
-        case 1: hipLaunchKernelGGL((hb::attention_values_kernel<GT, 1>), grid, block, 0, stream, a); break;
-        case 2: hipLaunchKernelGGL((hb::attention_values_kernel<GT, 2>), grid, block, 0, stream, a); break;
-        case 3: hipLaunchKernelGGL((hb::attention_values_kernel<GT, 3>), grid, block, 0, stream, a); break;
-        default: hipLaunchKernelGGL((hb::attention_values_kernel<GT, 4>), grid, block, 0, stream, a); break;
-        }
+        hipLaunchKernelGGL(hb::attention_values_kernel<GT>, grid, block, 0, stream, a);
     });
 }
 
@@ -245,8 +243,8 @@ int hb_attention(const hb_cache *cache, const int64_t *q0, const int64_t *q1, si
             }
         }
         if (e == hipSuccess) {
-            const unsigned over = (unsigned)(((uint64_t)q_heads * cache->dim + hb::kAttentionBlock - 1) / hb::kAttentionBlock);
-            hipLaunchKernelGGL(hb::attention_join_kernel, dim3(over, (unsigned)batch), dim3(hb::kAttentionBlock), 0, (hipStream_t)stream, a);
+            const unsigned over = (unsigned)(((uint64_t)q_heads * cache->dim + hb::kJoinNumbers - 1) / hb::kJoinNumbers);
+            hipLaunchKernelGGL(hb::attention_join_kernel, dim3(over, (unsigned)batch), dim3(hb::kJoinBlock), 0, (hipStream_t)stream, a);
             e = hipGetLastError();
         }
         if (e != hipSuccess) return hb::fail_hip(e, "kernel launch");

@@ -25,7 +25,7 @@ __device__ __forceinline__ uint32_t length_of(const AttentionArgs &a, uint32_t b
     return n < 0 ? 0 : ((uint32_t)n > a.max_len ? a.max_len : (uint32_t)n);
 }
 
-constexpr int kAttentionBlock = 256, kAttentionWaves = kAttentionBlock / 64;
+constexpr int kAttentionBlock = 512, kAttentionWaves = kAttentionBlock / 64, kJoinBlock = 256;
 
 // Both products of attention are sums of Beaver products of few fresh vectors with many masked numbers D = x - b of the cache.  With a = a_0 + a_1 and
 // eps = (q or p) - a the two parties' sums are, their terms collected by what is read from the cache or drawn for it,
@@ -38,6 +38,9 @@ constexpr int kAttentionBlock = 256, kAttentionWaves = kAttentionBlock / 64;
 // of v, nothing where s < i: 16 GT columns, GT tiles.  The vectors' digits lie in LDS as planes [digit][v], the columns of digit i
 // are the planes 2 GT i further up, and planes of zeros lie before the first; a tile whose columns all have s < i is left out (36 of 64
 // products at GT = 8, 20 of 32 at GT = 4).  int32 sums hold 2^17 a place: 2^14 places at most go into one.
+//
+// The matrices' words go in with their bytes' top bits flipped, which is a number less 0x80..80: every vector's result is owed that constant times the sum of
+// its entries over the three matrices (owed[v]).
 constexpr int kZeroPlanes = 16, kMostPlaces = 1 << 14;
 
 template <int GT>
@@ -59,7 +62,7 @@ __device__ __forceinline__ void store_vector(uint8_t *planes, uint32_t stride, u
 // The vectors of one query head for the three matrices.
 template <int GT>
 __device__ __forceinline__ void store_vectors(uint8_t *lds, uint32_t stride, uint32_t head, uint32_t at, const uint64_t (&eps)[4], const uint64_t (&a0)[4],
-                                              const uint64_t (&a1)[4])
+                                              const uint64_t (&a1)[4], unsigned long long *owed)
 {
     const uint32_t matrix = Vectors<GT>::planes * stride;
     uint64_t v[4];
@@ -74,16 +77,22 @@ __device__ __forceinline__ void store_vectors(uint8_t *lds, uint32_t stride, uin
     for (int j = 0; j < 4; ++j) v[j] = eps[j] + a0[j];
     store_vector<GT>(lds + 2 * matrix, stride, head, at, v);
     store_vector<GT>(lds + 2 * matrix, stride, GT + head, at, a1);
+    uint64_t sum_eps = 0, sum0 = 0, sum1 = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum_eps += eps[j], sum0 += a0[j], sum1 += a1[j];
+    atomicAdd(&owed[head], (unsigned long long)(kDigitBias * (2 * sum_eps + sum0)));
+    atomicAdd(&owed[GT + head], (unsigned long long)(kDigitBias * (2 * sum0 + 3 * sum1 + sum_eps)));
 }
 
 // Zeros where no vector is: before the planes, and party 0's vectors for b_1.
 template <int GT>
-__device__ __forceinline__ void clear_planes(uint8_t *lds, uint32_t stride)
+__device__ __forceinline__ void clear_planes(uint8_t *lds, uint32_t stride, unsigned long long *owed, uint32_t threads)
 {
+    if (threadIdx.x < 2 * GT) owed[threadIdx.x] = 0;
     const uint32_t matrix = Vectors<GT>::planes * stride, words = stride / 4;
-    for (uint32_t i = threadIdx.x; i < 3 * kZeroPlanes * words; i += kAttentionBlock)
+    for (uint32_t i = threadIdx.x; i < 3 * kZeroPlanes * words; i += threads)
         *reinterpret_cast<uint32_t *>(lds + i / (kZeroPlanes * words) * matrix + i % (kZeroPlanes * words) * 4) = 0;
-    for (uint32_t i = threadIdx.x; i < 8 * GT * words; i += kAttentionBlock) {
+    for (uint32_t i = threadIdx.x; i < 8 * GT * words; i += threads) {
         const uint32_t plane = i / words;
         *reinterpret_cast<uint32_t *>(lds + matrix + (kZeroPlanes + plane / GT * Vectors<GT>::nv + plane % GT) * stride + i % words * 4) = 0;
     }
@@ -110,14 +119,63 @@ __device__ __forceinline__ void multiply(i32x4_t (&sums)[GT], const MatrixDigits
 __device__ __forceinline__ void digits_at(MatrixDigits &d, int s, const uint64_t (&v)[4])
 {
     uint32_t w[8];
-    digits_of(v, w);
+    digits_of_flipped(v, w);
 #pragma unroll
     for (int i = 0; i < 8; ++i) d[i][s] = w[i];
 }
 
+// Digits of 16 dealer words, state(j) that of word j, eight in step (four: 1 to 4 % slower; 16: as fast).
+template <class State>
+__device__ __forceinline__ void draw_digits(MatrixDigits &d, const State &state)
+{
+    constexpr int IN_STEP = 8;
+#pragma unroll
+    for (int s = 0; s < 4; s += IN_STEP / 4) {
+        uint64_t z[IN_STEP];
+#pragma unroll
+        for (int j = 0; j < IN_STEP; ++j) z[j] = state(4 * s + j);
+        mix_flipped<true>(z);
+#pragma unroll
+        for (int x = 0; x < IN_STEP / 4; ++x) digits_at(d, s + x, {z[4 * x], z[4 * x + 1], z[4 * x + 2], z[4 * x + 3]});
+    }
+}
+__device__ __forceinline__ void masked_digits(MatrixDigits &d, const uint64_t (&delta)[16])
+{
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+        digits_at(d, s, {delta[4 * s] ^ kDigitBias, delta[4 * s + 1] ^ kDigitBias, delta[4 * s + 2] ^ kDigitBias, delta[4 * s + 3] ^ kDigitBias});
+}
+
+// sums += the three matrices, 16 numbers a lane each, times their vectors: numbers(x) loads D, words(p, d) draws the digits of b_p.
+// EARLY: the loads are under way while words are drawn.  That holds 32 registers more: where they are there (128 for four wavefronts a SIMD)
+// it is 10 to 20 % faster (scores of 1111 positions at dim 80 24 us instead of 31), where they are not, spills cost more (values with
+// GT = 4, 32768 positions 115 instead of 96).
+template <int GT, bool EARLY, class Numbers, class Words>
+__device__ __forceinline__ void multiply_three(i32x4_t (&sums)[GT], const uint8_t *column, uint32_t matrix, uint32_t stride, const Numbers &numbers,
+                                               const Words &words)
+{
+    uint64_t delta[16];
+    MatrixDigits d;
+    auto masked = [&] {
+        masked_digits(d, delta);
+        multiply<GT>(sums, d, column + 2 * matrix, stride);
+    };
+    numbers(delta);
+    if constexpr (!EARLY) {
+        masked();
+        __builtin_amdgcn_sched_barrier(0);                    // D leaves its registers before words are drawn
+    }
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        words(p, d);
+        multiply<GT>(sums, d, column + p * matrix, stride);
+    }
+    if constexpr (EARLY) masked();
+}
+
 // The weights 2^(8s) put together: value[r] of vector v = lane mod 2 GT and row 4 (lane / 16) + r, in all lanes with that v.
 template <int GT>
-__device__ __forceinline__ void join_digits(const i32x4_t (&sums)[GT], uint32_t lane, uint64_t (&value)[4])
+__device__ __forceinline__ void join_digits(const i32x4_t (&sums)[GT], uint32_t lane, const unsigned long long *owed, uint64_t (&value)[4])
 {
     constexpr int kPer = 16 / Vectors<GT>::nv;                 // values of s in a tile
     // 2^(8 s') of this lane's s' = s mod kPer
@@ -132,7 +190,7 @@ __device__ __forceinline__ void join_digits(const i32x4_t (&sums)[GT], uint32_t 
         if constexpr (kPer > 1) y *= weight;
 #pragma unroll
         for (int step = Vectors<GT>::nv; step < 16; step *= 2) y += __shfl_xor((unsigned long long)y, step, 64);
-        value[r] = y;
+        value[r] = y + owed[lane % Vectors<GT>::nv];
     }
 }
 
@@ -160,17 +218,18 @@ __device__ __forceinline__ HeadChunk head_chunk(const AttentionArgs &a, uint32_t
 // Scores.  A wavefront takes 16 positions at a time: a row of its tile is a key, lane l has row l mod 16 and of every 64 dimensions the pairs
 // 8 j + 2 (l / 16), j = 0 .. 7 (the lanes of a row read 64 bytes side by side).
 template <int GT, int ND>
-__global__ void __launch_bounds__(kAttentionBlock)
+__global__ void __launch_bounds__(kAttentionBlock, 4)
 attention_scores_kernel(AttentionArgs a)
 {
     constexpr uint32_t kStride = 64 * ND + 16;
     __shared__ __align__(16) uint8_t lds[3 * Vectors<GT>::planes * kStride];
+    __shared__ unsigned long long owed[2 * GT];
     const CacheView &c = a.cache;
     const HeadChunk h = head_chunk<GT>(a, blockIdx.x);
     const uint32_t first = blockIdx.y * a.per_scores, length = __builtin_amdgcn_readfirstlane(length_of(a, h.b));
     const uint32_t end = first + a.per_scores < a.max_len ? first + a.per_scores : a.max_len;
     const uint64_t row0 = (uint64_t)h.b * a.q_heads + h.first;
-    if (first >= length) {                                    // all of it behind the sequence's end
+    if (first >= length || c.pages == 0) {                    // all of it behind the sequence's end
         const uint32_t count = end - first;
         for (uint32_t i = threadIdx.x; i < h.count * count; i += kAttentionBlock) {
             const uint64_t j = (row0 + i / count) * a.max_len + first + i % count;
@@ -179,7 +238,8 @@ attention_scores_kernel(AttentionArgs a)
         }
         return;
     }
-    clear_planes<GT>(lds, kStride);
+    clear_planes<GT>(lds, kStride, owed, kAttentionBlock);
+    __syncthreads();
     for (uint32_t i = threadIdx.x; i < GT * ND * 16; i += kAttentionBlock) {
         const uint32_t head = i / (ND * 16), piece = i / 4 % (4 * ND), g = i % 4;          // four dimensions: pairs of two j
         const uint32_t d0 = 16 * piece + 2 * g;
@@ -194,53 +254,51 @@ attention_scores_kernel(AttentionArgs a)
             a1[j] = there ? mix64(z + kGamma) : 0;
             eps[j] = there ? (a.q[0][at] - a0[j]) + (a.q[1][at] - a1[j]) : 0;              // opened
         }
-        store_vectors<GT>(lds, kStride, head, piece / 4 * 64 + 16 * g + piece % 4 * 4, eps, a0, a1);
+        store_vectors<GT>(lds, kStride, head, piece / 4 * 64 + 16 * g + piece % 4 * 4, eps, a0, a1, owed);
     }
     __syncthreads();
     const uint32_t lane = threadIdx.x % 64, g = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint8_t *column = lds + (lane % 16) * kStride + 16 * g;
     constexpr uint32_t kMatrix = Vectors<GT>::planes * kStride;
+    const uint32_t chunks = (c.dim + 63) / 64;
     for (uint32_t t0 = first + 16 * wave; t0 < end; t0 += 16 * kAttentionWaves) {
         const uint32_t t = t0 + lane % 16;
         const int64_t page = page_of(a, h.b, t, length);
-        const bool there = page >= 0;
-        const uint64_t place = place_in_page(c, h.head, t % c.page, 2 * g);
-        const uint64_t *keys = c.keys + (there ? page * page_numbers(c) + place : 0);
-        const uint64_t z0 = state_of(there ? stream_word(c.page_seeds[page], 0) : 0, 2 * place);
+        const uint64_t there = __ballot(page >= 0);
+        // A row without a key reads the first one's: its score is not used.
+        const uint64_t place = page >= 0 ? place_in_page(c, h.head, t % c.page, 0) : 0;
+        const uint64_t *keys = c.keys + (page >= 0 ? page : 0) * page_numbers(c) + place;
+        uint64_t z0 = state_of(stream_word(c.page_seeds[page >= 0 ? page : 0], 0), 2 * (place + 2 * g));
         i32x4_t sums[GT] = {};
+        const uint8_t *at = column;
+#pragma unroll 1
+        for (uint32_t chunk = 0; chunk < chunks; ++chunk) {
+            auto numbers = [&](uint64_t (&delta)[16]) {
 #pragma unroll
-        for (int chunk = 0; chunk < ND; ++chunk) {
-            uint64_t delta[16];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                U64x2 v{0, 0};
-                if (there && 64 * chunk + 8 * j + 2 * g < c.dim) v = load_stream2(keys + 64 * chunk + 8 * j);
-                delta[2 * j] = v.a;
-                delta[2 * j + 1] = v.b;
-            }
-            MatrixDigits d;
-#pragma unroll
-            for (int p = 0; p < 2; ++p) {
-#pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    uint64_t b[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) b[j] = mix64(z0 + (uint64_t)(2 * (64 * chunk + 8 * (2 * s + j / 2) + j % 2) + p) * kGamma);
-                    digits_at(d, s, b);
+                for (int j = 0; j < 8; ++j) {
+                    uint32_t dim = 64 * chunk + 8 * j + 2 * g;
+                    dim = dim < c.dim ? dim : c.dim - 2;          // behind the last dimension the vectors are zeros
+                    const U64x2 v = load_stream2(keys + dim);
+                    delta[2 * j] = v.a;
+                    delta[2 * j + 1] = v.b;
                 }
-                multiply<GT>(sums, d, column + p * kMatrix + 64 * chunk, kStride);
-            }
-#pragma unroll
-            for (int s = 0; s < 4; ++s) digits_at(d, s, {delta[4 * s], delta[4 * s + 1], delta[4 * s + 2], delta[4 * s + 3]});
-            multiply<GT>(sums, d, column + 2 * kMatrix + 64 * chunk, kStride);
+            };
+            auto words = [&](int p, MatrixDigits &d) {
+                draw_digits(d, [&](int j) { return z0 + (uint64_t)(2 * (8 * (j / 2) + j % 2) + p) * kGamma; });
+            };
+            multiply_three<GT, (GT <= 4)>(sums, at, kMatrix, kStride, numbers, words);
+            z0 += 128 * kGamma;
+            at += 64;
         }
         uint64_t mine[4], other[4];
-        join_digits<GT>(sums, lane, mine);
+        join_digits<GT>(sums, lane, owed, mine);
 #pragma unroll
         for (int r = 0; r < 4; ++r) other[r] = __shfl_xor((unsigned long long)mine[r], GT, 64);
         // The lanes of a head share out its four rows.
-        const bool party1 = (lane & GT) != 0;
-        const uint32_t head = lane % GT, part = lane % 16 / GT;
+        uint32_t l = lane;
+        settle(l);                                            // (nothing of this stays in registers from tile to tile)
+        const bool party1 = (l & GT) != 0;
+        const uint32_t head = l % GT, part = l % 16 / GT;
         constexpr int kRows = GT == 8 ? 2 : 1;
         if (part * kRows < 4 && head < h.count) {
 #pragma unroll
@@ -251,11 +309,11 @@ attention_scores_kernel(AttentionArgs a)
                     if (part * kRows + x == r) y = Pair{mine[r], other[r]};
                 }
                 if (party1) y = Pair{y.p1, y.p0};
-                const uint32_t at = t0 + 4 * g + part * kRows + x;
+                const uint32_t at = t0 + 4 * (l / 16) + part * kRows + x;
                 if (at >= end) continue;
                 const uint64_t j = (row0 + head) * a.max_len + at;
                 Pair score{0, 0};
-                if (page_of(a, h.b, at, length) >= 0) {
+                if ((uint32_t)there >> (at - t0) & 1) {
                     const uint64_t z = state_of(a.seed_s, 5 * j), c0 = mix64(z);
                     score = truncate_drawn(Pair{y.p0 + c0, y.p1 - c0}, 16, z + kGamma);
                 }
@@ -266,16 +324,18 @@ attention_scores_kernel(AttentionArgs a)
     }
 }
 
-// The product with the values.  A row of a wavefront's tile is a dimension (DT tiles of 16), lane l takes 16 of every 64 positions; the workgroup makes
-// the weights' vectors of 128 positions at a time.
+// The product with the values.  A wavefront has 16 dimensions, the rows of its tile, and lane l takes 16 of every 64 positions; the workgroup, up to 128 dimensions,
+// makes the weights' vectors of 128 positions at a time.
 constexpr int kValueChunk = 128;
 
-template <int GT, int DT>
-__global__ void __launch_bounds__(kAttentionBlock)
+template <int GT>
+__global__ void __launch_bounds__(kAttentionBlock, 4)
 attention_values_kernel(AttentionArgs a)
 {
+    const uint32_t threads = blockDim.x;                      // 64 for every 16 dimensions
     constexpr uint32_t kStride = kValueChunk + 16;
     __shared__ __align__(16) uint8_t lds[3 * Vectors<GT>::planes * kStride];
+    __shared__ unsigned long long owed[2 * GT];
     __shared__ uint64_t row_at[kValueChunk], row_state[kValueChunk];       // a position's numbers and masks
     const CacheView &c = a.cache;
     const HeadChunk h = head_chunk<GT>(a, blockIdx.x);
@@ -286,16 +346,21 @@ attention_values_kernel(AttentionArgs a)
     const uint32_t lane = threadIdx.x % 64, g = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint8_t *column = lds + (lane % 16) * kStride + 16 * g;
     constexpr uint32_t kMatrix = Vectors<GT>::planes * kStride;
-    clear_planes<GT>(lds, kStride);
-    i32x4_t sums[DT][GT] = {};
+    clear_planes<GT>(lds, kStride, owed, threads);
+    __syncthreads();
+    const uint32_t dim0 = blockIdx.z * (kAttentionWaves * 16) + 16 * wave, dim = dim0 + lane % 16 < c.dim ? dim0 + lane % 16 : 0;
+    const uint64_t z = (uint64_t)(2 * dim) * kGamma;
+    i32x4_t sums[GT] = {};
     for (uint32_t t0 = first; t0 < end; t0 += kValueChunk) {
-        for (uint32_t i = threadIdx.x; i < kValueChunk; i += kAttentionBlock) {
+        uint32_t thread = threadIdx.x;
+        settle(thread);                                       // what follows from it is not kept in registers from chunk to chunk
+        for (uint32_t i = thread; i < kValueChunk; i += threads) {
             const int64_t page = page_of(a, h.b, t0 + i, end);
             const uint64_t place = place_in_page(c, h.head, (t0 + i) % c.page, 0);
-            row_at[i] = page >= 0 ? page * page_numbers(c) + place : ~0ull;
+            row_at[i] = page >= 0 ? page * page_numbers(c) + place : 0;       // without a value: the first one's, times zeros
             row_state[i] = page >= 0 ? state_of(stream_word(c.page_seeds[page], 1), 2 * place) : 0;
         }
-        for (uint32_t i = threadIdx.x; i < GT * kValueChunk / 4; i += kAttentionBlock) {
+        for (uint32_t i = thread; i < GT * kValueChunk / 4; i += threads) {
             const uint32_t head = i / (kValueChunk / 4), at = i % (kValueChunk / 4) * 4;
             uint64_t eps[4], a0[4], a1[4];
 #pragma unroll
@@ -307,74 +372,68 @@ attention_values_kernel(AttentionArgs a)
                 a1[j] = there ? mix64(z + kGamma) : 0;
                 eps[j] = there ? (a.scores[0][n] - a0[j]) + (a.scores[1][n] - a1[j]) : 0;  // opened
             }
-            store_vectors<GT>(lds, kStride, head, at, eps, a0, a1);
+            store_vectors<GT>(lds, kStride, head, at, eps, a0, a1, owed);
         }
         __syncthreads();
-        for (uint32_t block = 0; block < kValueChunk / 64 && t0 + 64 * block < end; ++block) {
+        for (uint32_t block = 0; block < kValueChunk / 64 && t0 + 64 * block < end && c.pages != 0; ++block) {
+auto numbers = [&](uint64_t (&delta)[16]) {
 #pragma unroll
-            for (int tile = 0; tile < DT; ++tile) {
-                const uint32_t dim = 16 * (wave * DT + tile) + lane % 16;
-                if (16 * (wave * DT + tile) >= c.dim) continue;
-                uint64_t delta[16], z[16];
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const uint64_t at = row_at[64 * block + 16 * g + j];
-                    z[j] = row_state[64 * block + 16 * g + j] + (uint64_t)(2 * dim) * kGamma;
-                    delta[j] = at != ~0ull && dim < c.dim ? load_stream(c.values + at + dim) : 0;
-                }
-                MatrixDigits d;
-#pragma unroll
-                for (int p = 0; p < 2; ++p) {
-#pragma unroll
-                    for (int s = 0; s < 4; ++s) {
-                        uint64_t b[4];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) b[j] = mix64(z[4 * s + j] + (uint64_t)p * kGamma);
-                        digits_at(d, s, b);
-                    }
-                    multiply<GT>(sums[tile], d, column + p * kMatrix + 64 * block, kStride);
-                }
-#pragma unroll
-                for (int s = 0; s < 4; ++s) digits_at(d, s, {delta[4 * s], delta[4 * s + 1], delta[4 * s + 2], delta[4 * s + 3]});
-                multiply<GT>(sums[tile], d, column + 2 * kMatrix + 64 * block, kStride);
-            }
+                for (int j = 0; j < 16; ++j) delta[j] = load_stream(c.values + row_at[64 * block + 16 * g + j] + dim);
+            };
+            auto words = [&](int p, MatrixDigits &d) {
+                draw_digits(d, [&](int j) { return row_state[64 * block + 16 * g + j] + (z + (uint64_t)p * kGamma); });
+            };
+            multiply_three<GT, (GT <= 2)>(sums, column + 64 * block, kMatrix, kStride, numbers, words);
         }
         __syncthreads();
     }
     // One partial sum for each number of the output and party, in lanes of the first half of a tile's columns that hold it.
     const uint64_t numbers = (uint64_t)a.batch * a.q_heads * c.dim;
-    const uint32_t head = lane % GT;
-    const uint64_t party = (lane & GT) != 0;
+    uint32_t column_of = lane;
+    settle(column_of);
+    const uint32_t head = column_of % GT;
+    const uint64_t party = (column_of & GT) != 0;
+uint64_t y[4];
+    join_digits<GT>(sums, lane, owed, y);
+    if (lane % 16 >= Vectors<GT>::nv || head >= h.count) return;
 #pragma unroll
-    for (int tile = 0; tile < DT; ++tile) {
-        uint64_t y[4];
-        join_digits<GT>(sums[tile], lane, y);
-        if (lane % 16 >= Vectors<GT>::nv || head >= h.count) continue;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const uint32_t dim = 16 * (wave * DT + tile) + 4 * g + r;
-            if (dim < c.dim) a.parts[(2 * (uint64_t)blockIdx.y + party) * numbers + (row0 + head) * c.dim + dim] = y[r];
-        }
+    for (int r = 0; r < 4; ++r) {
+        const uint32_t to = dim0 + 4 * g + r;
+        if (to < c.dim) a.parts[(2 * (uint64_t)blockIdx.y + party) * numbers + (row0 + head) * c.dim + to] = y[r];
     }
 }
 
-// Joins the splits and divides by the length: a truncation by its whole bits, a factor in (1/2, 1] for the rest.
-__global__ void __launch_bounds__(kAttentionBlock)
+// Joins the splits and divides by the length: a truncation by its whole bits, a factor in (1/2, 1] for the rest.  32 numbers a workgroup, whose
+// splits eight threads each share out.
+constexpr int kJoinNumbers = 32, kJoinShares = kJoinBlock / kJoinNumbers;
+
+__global__ void __launch_bounds__(kJoinBlock)
 attention_join_kernel(AttentionArgs a)
 {
+    __shared__ uint64_t partial[2][kJoinShares][kJoinNumbers];
     const uint64_t per = (uint64_t)a.q_heads * a.cache.dim;
-    const uint32_t b = blockIdx.y, at = blockIdx.x * kAttentionBlock + threadIdx.x;
-    if (at >= per) return;
+    const uint32_t b = blockIdx.y, x = threadIdx.x % kJoinNumbers, share = threadIdx.x / kJoinNumbers, at = blockIdx.x * kJoinNumbers + x;
     const uint64_t i = b * per + at, numbers = a.batch * per;
     const uint32_t length = __builtin_amdgcn_readfirstlane(length_of(a, b));
+    const uint32_t splits = (length + a.per_split - 1) / a.per_split;
     Pair o{0, 0};
+    if (at < per) {
+        for (uint32_t s = share; s < splits; s += kJoinShares) {
+            o.p0 += a.parts[2 * (uint64_t)s * numbers + i];
+            o.p1 += a.parts[(2 * (uint64_t)s + 1) * numbers + i];
+        }
+    }
+    partial[0][share][x] = o.p0;
+    partial[1][share][x] = o.p1;
+    __syncthreads();
+    if (share != 0 || at >= per) return;
     if (length != 0) {
         const uint64_t z = state_of(a.seed_o, 9 * i), c0 = mix64(z);
         o = Pair{c0, 0 - c0};
-        const uint32_t splits = (length + a.per_split - 1) / a.per_split;
-        for (uint32_t s = 0; s < splits; ++s) {
-            o.p0 += a.parts[2 * (uint64_t)s * numbers + i];
-            o.p1 += a.parts[(2 * (uint64_t)s + 1) * numbers + i];
+#pragma unroll
+        for (int s = 0; s < kJoinShares; ++s) {
+            o.p0 += partial[0][s][x];
+            o.p1 += partial[1][s][x];
         }
         const int whole = 31 - __builtin_clz(length);
         const uint64_t factor = ((1ull << (16 + whole)) + length / 2) / length;

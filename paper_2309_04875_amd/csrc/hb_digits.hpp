@@ -26,6 +26,56 @@ __device__ __forceinline__ void turn_bytes(const uint32_t (&w)[4], uint32_t *out
     out[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
 }
 
+// Digits of four words whose bytes have their top bits flipped already, of v - 0x8080808080808080 that is: one addition less for each number
+// where sums of such digits with a vector are owed 0x8080808080808080 times the vector's sum, once for all of them.
+__device__ __forceinline__ void digits_of_flipped(const uint64_t (&v)[4], uint32_t (&out)[8])
+{
+    const uint32_t low[4] = {(uint32_t)v[0], (uint32_t)v[1], (uint32_t)v[2], (uint32_t)v[3]};
+    const uint32_t high[4] = {(uint32_t)(v[0] >> 32), (uint32_t)(v[1] >> 32), (uint32_t)(v[2] >> 32), (uint32_t)(v[3] >> 32)};
+    turn_bytes(low, out);
+    turn_bytes(high, out + 4);
+}
+
+// Dealer words of N states with the top bits of their bytes flipped; the last xor of the generator takes the flip along.
+template <bool RUNS, int N>
+__device__ __forceinline__ void mix_flipped(uint64_t (&z)[N])
+{
+    auto last = [&](uint64_t (&t)[N]) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = bitop3<kTtXor3>(z[i], t[i], kDigitBias);
+    };
+    uint64_t t[N];
+    if constexpr (RUNS) {                                      // as in mix_words
+        settle(z);
+        priority<true, kElsewhere>();
+        xor_shift(z, 30);
+        settle(z);
+        priority<true, kElsewhere>();
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] *= 0xBF58476D1CE4E5B9ull;
+        xor_shift(z, 27);
+        settle(z);
+        priority<true, kElsewhere>();
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] *= 0x94D049BB133111EBull;
+#pragma unroll
+        for (int i = 0; i < N; ++i) t[i] = z[i] >> 31;
+        settle(t);
+        priority<true, kXorRuns>();
+        last(t);
+        settle(z);
+        priority<true, kElsewhere>();
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            z[i] = (z[i] ^ (z[i] >> 30)) * 0xBF58476D1CE4E5B9ull;
+            z[i] = (z[i] ^ (z[i] >> 27)) * 0x94D049BB133111EBull;
+            t[i] = z[i] >> 31;
+        }
+        last(t);
+    }
+}
+
 // Digits of four numbers: out[i] holds digit i of v[0] .. v[3], one byte each.
 __device__ __forceinline__ void digits_of(const uint64_t (&v)[4], uint32_t (&out)[8])
 {
