@@ -4,25 +4,59 @@
 
 namespace {
 
-template <int TM, int RT, int WN, int WK, int FLUSH>
+template <int TM, int RT, int WN, int WK, int P, int FLUSH>
 hipError_t go(hb::LinearArgs &a, hipStream_t stream)
 {
     const uint64_t tiles = ((uint64_t)a.outs + 16 * WN * RT - 1) / (16 * WN * RT);
     a.row_tiles = (a.rows + TM - 1) / TM;
     const uint64_t blocks = tiles * a.row_tiles;
     if (blocks > 0x7fffffffull) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((hb::linear_q4_kernel<TM, RT, WN, WK, FLUSH>), dim3((unsigned)blocks), dim3(64 * WN * WK), 0, stream, a);
+    hipLaunchKernelGGL((hb::linear_q4_kernel<TM, RT, WN, WK, P, FLUSH>), dim3((unsigned)blocks), dim3(64 * WN * WK), 0, stream, a);
     return hipGetLastError();
 }
+
+// Which form a layer takes: the one whose rounds of 256 workgroups, one for each compute unit, cost least.  More rows and tiles of outputs in a
+// workgroup use its digits and weights more often, and fewer fill the chip.  A round's time in tenths of a us, measured at 4096 inputs in
+// groups of 128; all of them grow alike with the inputs, and in groups of 32 to about 2.5 times as much.  us by form, for rows x (inputs ->
+// outputs), the form taken in brackets:
+//               rows, tiles a workgroup:   1, 1    2, 1    2, 2    2, 4    4, 4    8, 4    8, 8
+//    1 x (4096 -> 4096)                   [6.1]    7.1     8.9    12.7    14.3    21.2    32.3
+//    2 x                                   9.8    [7.9]    9.5    13.4    14.8    21.2    32.3
+//    4 x                                  16.7    11.8   [10.0]   13.7    16.1    21.6    32.9
+//    8 x                                  29.7    20.3    17.9   [14.6]   16.6    23.6    32.7
+//   16 x                                  56.8    35.0    32.7    26.5   [17.8]   24.3    33.5
+//   32 x                                   110    63.3    61.9    48.6    32.1   [25.4]   34.5
+//   64 x                                   219     122     122    94.9    59.2    48.1   [37.3]
+//   64 x (4096 -> 16384)                   886     494     503     384     240     187    [116]
+//    8 x (512 -> 512)                      3.8    [4.1]    3.9     3.9     4.9     6.3     8.0
+// One row of many outputs (16384: 13.1 instead of 17.7) shares its digits among four tiles.
+struct Form {
+    uint64_t rows, tiles, round;
+};
+constexpr Form kForms[] = {{1, 1, 34}, {2, 1, 41}, {2, 2, 75}, {2, 4, 120}, {4, 4, 143}, {8, 4, 227}, {8, 8, 345}, {1, 4, 105}};
 
 template <int FLUSH>
 hipError_t by_shape(hb::LinearArgs &a, hipStream_t stream)
 {
-    const uint64_t wide = ((uint64_t)a.outs + 255) / 256 * ((a.rows + 3) / 4);
-    if (wide >= 512) return go<4, 4, 4, 1, FLUSH>(a, stream);
-    if (a.rows == 1) return go<1, 1, 1, 16, FLUSH>(a, stream);
-    if (a.rows == 2) return go<2, 1, 1, 8, FLUSH>(a, stream);
-    return go<4, 1, 1, 8, FLUSH>(a, stream);
+    const uint64_t tiles = ((uint64_t)a.outs + 15) / 16;
+    int best = 0;
+    uint64_t least = ~0ull;
+    for (int i = 0; i < (int)(sizeof(kForms) / sizeof(kForms[0])); ++i) {
+        const Form &f = kForms[i];
+        const uint64_t blocks = (a.rows + f.rows - 1) / f.rows * ((tiles + f.tiles - 1) / f.tiles), cost = (blocks + 255) / 256 * f.round;
+        if (cost < least) least = cost, best = i;
+    }
+    switch (best) {
+    case 0: return go<1, 1, 1, 16, 1, FLUSH>(a, stream);
+    case 1: return go<2, 1, 1, 8, 1, FLUSH>(a, stream);
+    case 2: return go<2, 1, 2, 8, 1, FLUSH>(a, stream);
+    case 3: return go<2, 1, 4, 4, 2, FLUSH>(a, stream);
+    // (eight wavefronts where scaling every 32 inputs takes more registers than sixteen leave: 16 x (4096 -> 4096) 39 instead of 58)
+    case 4: return go<4, 1, 4, FLUSH == 32 ? 2 : 4, 1, FLUSH>(a, stream);
+    case 5: return go<8, 1, 4, 2, 1, FLUSH>(a, stream);
+    case 6: return go<8, 1, 8, 1, 1, FLUSH>(a, stream);
+    default: return go<1, 1, FLUSH == 32 ? 1 : 4, FLUSH == 32 ? 16 : 4, FLUSH == 32 ? 1 : 4, FLUSH>(a, stream);
+    }
 }
 
 hipError_t launch(hb::LinearArgs &a, uint64_t group, hipStream_t stream)
