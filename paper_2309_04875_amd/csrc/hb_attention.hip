@@ -34,6 +34,18 @@ hb::CacheView view_of(const hb_cache *cache)
     return c;
 }
 
+// How the groups of numbers of all tokens go into workgroups; false: more than a grid holds.
+bool append_shape(size_t tokens, uint64_t groups, hb::AppendShape &shape)
+{
+    const uint64_t per = hb::kAppendBlock;
+    if (groups == 0) return true;
+    const uint64_t each = groups >= per ? (groups + per - 1) / per : 0, together = groups < per ? per / groups : 0;
+    const uint64_t blocks = each != 0 ? tokens * each : (tokens + together - 1) / together;
+    if (blocks > 0x7fffffffull) return false;
+    shape = hb::AppendShape{(uint32_t)blocks, (uint32_t)groups, (uint32_t)each, (uint32_t)together};
+    return true;
+}
+
 size_t round_up(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Workspace of hb_attention: shares of the scores, then the splits' partial sums.
@@ -166,10 +178,18 @@ int hb_cache_append(const hb_cache *cache, const int64_t *k0, const int64_t *k1,
         a.rot = (uint32_t)rot;
         a.frac = frac;
         a.q_mul = q_mul;
-        const uint64_t items = (2 * (uint64_t)cache->heads + q_heads) * (cache->dim / 2) * tokens;
-        const uint64_t blocks = (items + hb::kAppendBlock - 1) / hb::kAppendBlock;
+        // N = 2 from a workgroup for each compute unit on: below it a thread's time is the launch's (8 tokens of 48 heads of 128 4.5 us with N = 1, 5.0
+        // with 2; 333 of 36 heads of 80 9.5 and 8.8).
+        const uint64_t numbers = (uint64_t)tokens * (2 * (uint64_t)cache->heads + q_heads) * cache->dim;
+        const int n = rot % 4 == 0 && cache->dim % 4 == 0 && numbers >= 4ull * 256 * hb::kAppendBlock ? 2 : 1, groups = cache->dim / (2 * n);      // of a head
+        hb::AppendShape stored = {}, asked = {};
+        if (!append_shape(tokens, (uint64_t)cache->heads * groups, stored) || !append_shape(tokens, (uint64_t)q_heads * groups, asked)) return HB_EINVAL;
+        const uint64_t blocks = 2 * (uint64_t)stored.blocks + asked.blocks;
         if (blocks > 0x7fffffffull) return HB_EINVAL;
-        hipLaunchKernelGGL(hb::cache_append_kernel, dim3((unsigned)blocks), dim3(hb::kAppendBlock), 0, (hipStream_t)stream, a);
+        const uint32_t head_inverse = groups == 1 ? 0 : (uint32_t)(((1ull << 32) + groups - 1) / groups);
+        const dim3 grid((unsigned)blocks), block(hb::kAppendBlock);
+        if (n == 2) hipLaunchKernelGGL(hb::cache_append_kernel<2>, grid, block, 0, (hipStream_t)stream, a, stored, asked, head_inverse);
+        else hipLaunchKernelGGL(hb::cache_append_kernel<1>, grid, block, 0, (hipStream_t)stream, a, stored, asked, head_inverse);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return hb::fail_hip(e, "kernel launch");
     }

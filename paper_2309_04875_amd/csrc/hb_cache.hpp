@@ -2,6 +2,7 @@
 #pragma once
 
 #include "hb_fixed.hpp"
+#include "hb_kernels.hpp"
 
 namespace hb {
 
@@ -33,61 +34,144 @@ struct AppendArgs {
 
 constexpr int kAppendBlock = 256;
 
-// A thread takes a pair of numbers of one token: dimensions d and d + rot/2 of a rotated pair, two neighbours elsewhere.
+// What bounds it: HBM (24 bytes a key or value, 32 a query), and beside it vector-ALU issue: a rotated number takes four dealer words for its
+// truncation, and every number of the cache two for its mask, 18 instructions each.  A thread takes N neighbours (dimensions d ..) and the N that
+// turn with them (d + rot/2 ..; the next N elsewhere), so that both multiply the same row of the tables and a number's words are drawn in step;
+// N = 2 (16-byte accesses, half the addresses) where the rotated part and the rest divide into such groups: 2048 tokens of 8 + 8 + 32
+// heads of 128, 370 MB, in 76 us (4.9 TB/s) instead of 80.  Keys, values and queries have workgroups of their own, whose wavefronts then do the same.  The groups of a token are
+// shared out to workgroups, or
+// several tokens with few share one.
+struct AppendShape {
+    uint32_t blocks;            // of this kind (keys, values or queries)
+    uint32_t groups;            // of 2 N numbers of a token
+    uint32_t per_token;         // workgroups of a token, or 0:
+    uint32_t together;          // tokens of a workgroup
+};
+
+// N neighbouring numbers of both parties.
+template <int N>
+__device__ __forceinline__ void load_numbers(const uint64_t *const (&x)[2], uint64_t at, Pair (&y)[N])
+{
+    if constexpr (N == 2) {
+        const U64x2 a = load_stream2(x[0] + at), b = load_stream2(x[1] + at);
+        y[0] = Pair{a.a, b.a};
+        y[1] = Pair{a.b, b.b};
+    } else {
+        y[0] = Pair{load_stream(x[0] + at), load_stream(x[1] + at)};
+    }
+}
+template <int N>
+__device__ __forceinline__ void store_numbers(uint64_t *to, const uint64_t (&v)[N])
+{
+    if constexpr (N == 2) store_stream2(to, U64x2{v[0], v[1]});
+    else store_stream(to, v[0]);
+}
+
+// Truncations of N numbers, z: state of the first's first word.
+template <int N>
+__device__ __forceinline__ void truncate_numbers(Pair (&y)[N], int f, uint64_t z)
+{
+    uint64_t v[N * kTruncateWords];
+#pragma unroll
+    for (int j = 0; j < N * kTruncateWords; ++j) v[j] = z + (uint64_t)j * kGamma;
+    mix_words<true>(v);
+    settle(v);
+    priority<true, kElsewhere>();
+#pragma unroll
+    for (int j = 0; j < N; ++j) y[j] = truncate(y[j], f, v + kTruncateWords * j);
+}
+// What both parties learn of N numbers, z: state of the first's first mask word.
+template <int N>
+__device__ __forceinline__ void open_numbers(const Pair (&y)[N], uint64_t z, uint64_t *to)
+{
+    uint64_t b[2 * N], opened[N];
+#pragma unroll
+    for (int j = 0; j < 2 * N; ++j) b[j] = z + (uint64_t)j * kGamma;
+    mix_words<true>(b);
+    settle(b);
+    priority<true, kElsewhere>();
+#pragma unroll
+    for (int j = 0; j < N; ++j) opened[j] = (y[j].p0 - b[2 * j]) + (y[j].p1 - b[2 * j + 1]);
+    store_numbers<N>(to, opened);
+}
+
+template <int N>
 __global__ void __launch_bounds__(kAppendBlock)
-cache_append_kernel(AppendArgs a)
+cache_append_kernel(AppendArgs a, AppendShape stored, AppendShape asked, uint32_t head_inverse)
 {
     const CacheView &c = a.cache;
-    const uint32_t half = a.rot / 2, pairs = c.dim / 2;
-    const uint32_t items = (2 * c.heads + a.q_heads) * pairs;
-    const uint64_t i = (uint64_t)blockIdx.x * kAppendBlock + threadIdx.x;
-    const uint64_t token = i / items;
+    // Keys, then values, then queries.
+    uint32_t block = blockIdx.x;
+    const uint32_t kind = block < stored.blocks ? 0 : block < 2 * stored.blocks ? 1 : 2;
+    block -= kind * stored.blocks;
+    const AppendShape &shape = kind == 2 ? asked : stored;
+    const uint32_t heads = kind == 2 ? a.q_heads : c.heads, half = a.rot / 2, groups = c.dim / (2 * N);       // of a head
+    uint64_t token;
+    uint32_t item;
+    if (shape.per_token != 0) {
+        token = block / shape.per_token;
+        item = block % shape.per_token * kAppendBlock + threadIdx.x;
+        if (item >= shape.groups) return;
+    } else {
+        const uint32_t own = threadIdx.x / shape.groups;
+        if (own >= shape.together) return;
+        token = (uint64_t)block * shape.together + own;
+        item = threadIdx.x % shape.groups;
+    }
     if (token >= a.tokens) return;
-    const uint32_t item = (uint32_t)(i % items), pair = item % pairs;
-    uint32_t head = item / pairs;
-    const int64_t slot = a.slots[token];
+    const uint32_t head = groups == 1 ? item : __umulhi(item, head_inverse), group = item - head * groups;    // head_inverse: ceil(2^32 / groups)
+    const bool turned = kind != 1 && N * group < half;
+    const uint32_t d = kind == 1 ? 2 * N * group : turned ? N * group : a.rot + 2 * (N * group - half), apart = turned ? half : N;
+    const uint64_t *const x[2] = {kind == 0 ? a.k[0] : kind == 1 ? a.v[0] : a.q[0], kind == 0 ? a.k[1] : kind == 1 ? a.v[1] : a.q[1]};
+    const uint64_t at = (token * heads + head) * c.dim + d;
+    // All that depends on the token alone is under way before any of it is looked at.
+    const int64_t slot = a.slots[token], position = half != 0 ? a.positions[token] : 0;
+    Pair y0[N], y1[N];
+    load_numbers<N>(x, at, y0);
+    load_numbers<N>(x, at + apart, y1);
     if (slot < 0 || (uint64_t)slot >= (uint64_t)c.pages * c.page) return;
-    int64_t position = 0;
-    if (half != 0) {
-        position = a.positions[token];
-        if (position < 0 || (uint64_t)position >= a.table_rows) return;
-    }
-    const bool is_key = head < c.heads, is_query = head >= 2 * c.heads, turned = !is_query && !is_key ? false : pair < half;
-    if (!is_key) head -= is_query ? 2 * c.heads : c.heads;
-    const uint32_t d0 = pair < half && turned ? pair : (turned || !(is_key || is_query) ? 2 * pair : a.rot + 2 * (pair - half));
-    const uint32_t d1 = turned ? d0 + half : d0 + 1;
-    const uint64_t *const *x = is_query ? a.q : is_key ? a.k : a.v;
-    const uint64_t row = (token * (is_query ? a.q_heads : c.heads) + head) * c.dim;
-    Pair y0{x[0][row + d0], x[1][row + d0]}, y1{x[0][row + d1], x[1][row + d1]};
-    if (turned || is_query) {
-        uint64_t co = 1ull << a.frac, si = 0;
-        if (turned) {
-            co = (uint64_t)(int64_t)a.cos[position * half + pair];
-            si = (uint64_t)(int64_t)a.sin[position * half + pair];
+    if (half != 0 && (position < 0 || (uint64_t)position >= a.table_rows)) return;
+    if (turned || kind == 2) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            int64_t co = (int64_t)1 << a.frac, si = 0;
+            if (turned) {
+                co = a.cos[position * half + N * group + j];
+                si = a.sin[position * half + N * group + j];
+            }
+            if (kind == 2) {                         // the public factor goes into the table, rounded to its precision
+                const int64_t round = (int64_t)1 << (a.frac - 1);
+                co = (co * a.q_mul + round) >> a.frac;
+                si = (si * a.q_mul + round) >> a.frac;
+            }
+            const uint64_t cu = (uint64_t)co, su = (uint64_t)si;
+            const Pair u = y0[j], w = y1[j];
+            y0[j] = Pair{u.p0 * cu - w.p0 * su, u.p1 * cu - w.p1 * su};
+            y1[j] = Pair{w.p0 * cu + u.p0 * su, w.p1 * cu + u.p1 * su};
         }
-        if (is_query) {                              // the public factor goes into the table, rounded to its precision
-            const int64_t round = (int64_t)1 << (a.frac - 1);
-            co = (uint64_t)(((int64_t)co * a.q_mul + round) >> a.frac);
-            si = (uint64_t)(((int64_t)si * a.q_mul + round) >> a.frac);
-        }
-        const uint64_t base = is_query ? a.tokens * c.heads * c.dim : 0;
-        const Pair t0{y0.p0 * co - y1.p0 * si, y0.p1 * co - y1.p1 * si}, t1{y1.p0 * co + y0.p0 * si, y1.p1 * co + y0.p1 * si};
-        y0 = truncate_drawn(t0, a.frac, state_of(a.seedA, kTruncateWords * (base + row + d0)));
-        y1 = truncate_drawn(t1, a.frac, state_of(a.seedA, kTruncateWords * (base + row + d1)));
+        const uint64_t z = state_of(a.seedA, kTruncateWords * ((kind == 2 ? a.tokens * c.heads * c.dim : 0) + at));
+        truncate_numbers<N>(y0, a.frac, z);
+        truncate_numbers<N>(y1, a.frac, z + (uint64_t)(kTruncateWords * apart) * kGamma);
     }
-    if (is_query) {
-        a.qo[0][row + d0] = y0.p0;
-        a.qo[1][row + d0] = y0.p1;
-        a.qo[0][row + d1] = y1.p0;
-        a.qo[1][row + d1] = y1.p1;
+    if (kind == 2) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            uint64_t v0[N], v1[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                v0[j] = p == 0 ? y0[j].p0 : y0[j].p1;
+                v1[j] = p == 0 ? y1[j].p0 : y1[j].p1;
+            }
+            store_numbers<N>(a.qo[p] + at, v0);
+            store_numbers<N>(a.qo[p] + at + apart, v1);
+        }
         return;
     }
     const uint32_t page = (uint32_t)((uint64_t)slot / c.page), offset = (uint32_t)((uint64_t)slot % c.page);
-    const uint64_t masks = stream_word(c.page_seeds[page], is_key ? 0 : 1);
-    uint64_t *to = (is_key ? c.keys : c.values) + page * page_numbers(c);
-    const uint64_t e0 = place_in_page(c, head, offset, d0), e1 = place_in_page(c, head, offset, d1);
-    to[e0] = (y0.p0 - stream_word(masks, 2 * e0)) + (y0.p1 - stream_word(masks, 2 * e0 + 1));      // opened
-    to[e1] = (y1.p0 - stream_word(masks, 2 * e1)) + (y1.p1 - stream_word(masks, 2 * e1 + 1));
+    const uint64_t e = place_in_page(c, head, offset, d), z = state_of(stream_word(c.page_seeds[page], kind), 2 * e);
+    uint64_t *to = (kind == 0 ? c.keys : c.values) + page * page_numbers(c) + e;
+    open_numbers<N>(y0, z, to);
+    open_numbers<N>(y1, z + (uint64_t)(2 * apart) * kGamma, to + apart);
 }
 
 }  // namespace hb

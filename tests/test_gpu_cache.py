@@ -67,6 +67,14 @@ def test_tokens_and_heads(tokens, heads, q_heads):
     Case(rng, tokens, heads, q_heads, 32, 32, 7, tokens // 7 + 2).check()
 
 
+@pytest.mark.parametrize("dim,rot", [(128, 128), (128, 64), (80, 40), (64, 0), (20, 8), (12, 6), (66, 66)])
+def test_many_tokens(dim, rot):
+    """Launches that fill the chip, whose threads take four numbers each where the parts allow it."""
+    rng = np.random.default_rng(dim + rot)
+    tokens = 700000 // (16 * dim)
+    Case(rng, tokens, 3, 10, dim, rot, 16, tokens // 16 + 3).check()
+
+
 @pytest.mark.parametrize("page", [1, 3, 16, 64, 100])
 def test_pages(page):
     Case(np.random.default_rng(page), 40, 2, 2, 16, 8, page, 80 // page + 2).check()
