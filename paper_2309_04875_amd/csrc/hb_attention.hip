@@ -5,6 +5,9 @@
 
 #include <type_traits>
 
+#ifndef VC
+#define VC 0
+#endif
 namespace {
 
 // What a cache has to be, whatever is done with it.
@@ -76,13 +79,13 @@ AttentionLayout attention_layout(const hb_cache *cache, size_t batch, int q_head
 {
     AttentionLayout lay = {};
     const size_t scores = round_up(8 * batch * q_heads * max_len), numbers = batch * q_heads * cache->dim;
-    // Positions of a workgroup, a multiple of 128: what gives every compute unit two workgroups at a time, four where lengths may differ.
+    // Positions of a workgroup: what gives every compute unit two workgroups at a time, four where lengths may differ.
     const size_t some = batch != 0 ? batch : 1, groups = some * cache->heads * head_chunks(cache, q_heads), pieces = ((batch > 1 ? 1024 : 512) + groups - 1) / groups;
-    size_t per = ((max_len + pieces - 1) / pieces + 127) / 128 * 128;
+    size_t per = (max_len + pieces - 1) / pieces;
+    per = per > 64 ? (per + 127) / 128 * 128 : per > 32 ? 64 : per > 16 ? 32 : 16;
     if (per > hb::kMostPlaces) per = hb::kMostPlaces;
-    if (per < 128) per = 128;
     lay.per_scores = (uint32_t)per;
-    lay.per_split = (uint32_t)per;
+    lay.per_split = (uint32_t)(per < 64 ? 64 : per);
     lay.splits = (uint32_t)((max_len + lay.per_split - 1) / lay.per_split);
     lay.scores1 = scores;
     lay.parts = 2 * scores;
@@ -104,9 +107,10 @@ void with_heads(int together, const Body &body)
 
 void launch_scores(const hb::AttentionArgs &a, int together, dim3 grid, hipStream_t stream)
 {
+    const unsigned tiles = (a.per_scores + 15) / 16, most = hb::kAttentionWaves;
+    const dim3 block(64 * (tiles < most ? tiles : most));
     with_heads(together, [&](auto heads) {
         constexpr int GT = decltype(heads)::value;
-        const dim3 block(hb::kAttentionBlock);
         switch ((a.cache.dim + 63) / 64) {
         case 1: hipLaunchKernelGGL((hb::attention_scores_kernel<GT, 1>), grid, block, 0, stream, a); break;
         case 2: hipLaunchKernelGGL((hb::attention_scores_kernel<GT, 2>), grid, block, 0, stream, a); break;
@@ -123,7 +127,8 @@ void launch_values(const hb::AttentionArgs &a, int together, dim3 grid, hipStrea
     const dim3 block(64 * (grid.z > 1 ? most : tiles));
     with_heads(together, [&](auto heads) {
         constexpr int GT = decltype(heads)::value;
-        hipLaunchKernelGGL(hb::attention_values_kernel<GT>, grid, block, 0, stream, a);
+        if (GT == 8 || a.per_split <= 64 || VC) hipLaunchKernelGGL((hb::attention_values_kernel<GT, 64>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((hb::attention_values_kernel<GT, GT == 8 ? 64 : 128>), grid, block, 0, stream, a);
     });
 }
 
@@ -241,6 +246,7 @@ int hb_attention(const hb_cache *cache, const int64_t *q0, const int64_t *q1, si
         a.batch = (uint32_t)batch;
         a.q_heads = (uint32_t)q_heads;
         a.max_len = (uint32_t)max_len;
+        a.splits = lay.splits;
         a.per_scores = lay.per_scores;
         a.per_split = lay.per_split;
         const hb::GroupLauncher relu = hb::launcher_table().f[hb::kRelu][m - k - 1];
@@ -262,7 +268,7 @@ int hb_attention(const hb_cache *cache, const int64_t *q0, const int64_t *q1, si
                 e = hipGetLastError();
             }
         }
-        if (e == hipSuccess) {
+        if (e == hipSuccess && lay.splits != 1) {
             const unsigned over = (unsigned)(((uint64_t)q_heads * cache->dim + hb::kJoinNumbers - 1) / hb::kJoinNumbers);
             hipLaunchKernelGGL(hb::attention_join_kernel, dim3(over, (unsigned)batch), dim3(hb::kJoinBlock), 0, (hipStream_t)stream, a);
             e = hipGetLastError();

@@ -16,7 +16,7 @@ struct AttentionArgs {
     const int32_t *table, *lens;          // [batch][table_width], [batch]
     uint64_t table_width;
     uint64_t seed_q, seed_s, seed_p, seed_o;
-    uint32_t batch, q_heads, max_len, per_scores, per_split;    // positions of a workgroup
+    uint32_t batch, q_heads, max_len, splits, per_scores, per_split;    // per_..: positions of a workgroup
 };
 
 __device__ __forceinline__ uint32_t length_of(const AttentionArgs &a, uint32_t b)
@@ -49,39 +49,30 @@ struct Vectors {
     static constexpr bool used(int i, int tile) { return i * nv <= 16 * tile + 15; }
 };
 
-// Digits of four consecutive places of vector v, at byte `at` of its planes.
+// Digits of one place of vector v, four lanes side by side having four consecutive places, the first at byte `at` of its planes: a lane writes digits j
+// and 4 + j of all four, j = lane mod 4.
 template <int GT>
-__device__ __forceinline__ void store_vector(uint8_t *planes, uint32_t stride, uint32_t v, uint32_t at, const uint64_t (&x)[4])
+__device__ __forceinline__ void store_vector(uint8_t *planes, uint32_t stride, const QuadTurn &turn, uint32_t j, uint32_t v, uint32_t at, uint64_t x)
 {
-    uint32_t d[8];
-    digits_of(x, d);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) *reinterpret_cast<uint32_t *>(planes + (kZeroPlanes + j * Vectors<GT>::nv + v) * stride + at) = d[j];
+    x += kDigitBias;
+    uint8_t *to = planes + (kZeroPlanes + j * Vectors<GT>::nv + v) * stride + at;
+    *reinterpret_cast<uint32_t *>(to) = turn((uint32_t)x) ^ kDigitFlip;
+    *reinterpret_cast<uint32_t *>(to + 4 * Vectors<GT>::nv * stride) = turn((uint32_t)(x >> 32)) ^ kDigitFlip;
 }
 
-// The vectors of one query head for the three matrices.
+// The vectors of one query head for the three matrices, a place a lane; what is not there is zeros.
 template <int GT>
-__device__ __forceinline__ void store_vectors(uint8_t *lds, uint32_t stride, uint32_t head, uint32_t at, const uint64_t (&eps)[4], const uint64_t (&a0)[4],
-                                              const uint64_t (&a1)[4], unsigned long long *owed)
+__device__ __forceinline__ void store_vectors(uint8_t *lds, uint32_t stride, const QuadTurn &turn, uint32_t j, uint32_t head, uint32_t at, uint64_t eps,
+                                              uint64_t a0, uint64_t a1, unsigned long long *owed)
 {
     const uint32_t matrix = Vectors<GT>::planes * stride;
-    uint64_t v[4];
-    store_vector<GT>(lds, stride, head, at, eps);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = a0[j] + a1[j];
-    store_vector<GT>(lds, stride, GT + head, at, v);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] += eps[j];
-    store_vector<GT>(lds + matrix, stride, GT + head, at, v);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = eps[j] + a0[j];
-    store_vector<GT>(lds + 2 * matrix, stride, head, at, v);
-    store_vector<GT>(lds + 2 * matrix, stride, GT + head, at, a1);
-    uint64_t sum_eps = 0, sum0 = 0, sum1 = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) sum_eps += eps[j], sum0 += a0[j], sum1 += a1[j];
-    atomicAdd(&owed[head], (unsigned long long)(kDigitBias * (2 * sum_eps + sum0)));
-    atomicAdd(&owed[GT + head], (unsigned long long)(kDigitBias * (2 * sum0 + 3 * sum1 + sum_eps)));
+    store_vector<GT>(lds, stride, turn, j, head, at, eps);
+    store_vector<GT>(lds, stride, turn, j, GT + head, at, a0 + a1);
+    store_vector<GT>(lds + matrix, stride, turn, j, GT + head, at, a0 + a1 + eps);
+    store_vector<GT>(lds + 2 * matrix, stride, turn, j, head, at, eps + a0);
+    store_vector<GT>(lds + 2 * matrix, stride, turn, j, GT + head, at, a1);
+    const uint64_t owed0 = quad_sum(2 * eps + a0), owed1 = quad_sum(2 * a0 + 3 * a1 + eps);
+    if (j < 2) atomicAdd(&owed[j * GT + head], (unsigned long long)(kDigitBias * (j == 0 ? owed0 : owed1)));
 }
 
 // Zeros where no vector is: before the planes, and party 0's vectors for b_1.
@@ -165,7 +156,7 @@ __device__ __forceinline__ void multiply_three(i32x4_t (&sums)[GT], const uint8_
         masked();
         __builtin_amdgcn_sched_barrier(0);                    // D leaves its registers before words are drawn
     }
-#pragma unroll
+#pragma unroll 1
     for (int p = 0; p < 2; ++p) {
         words(p, d);
         multiply<GT>(sums, d, column + p * matrix, stride);
@@ -192,6 +183,35 @@ __device__ __forceinline__ void join_digits(const i32x4_t (&sums)[GT], uint32_t 
         for (int step = Vectors<GT>::nv; step < 16; step *= 2) y += __shfl_xor((unsigned long long)y, step, 64);
         value[r] = y + owed[lane % Vectors<GT>::nv];
     }
+}
+
+// After join_digits the lanes of a head, 16 / GT by four rows, hold all its rows: each takes one of them (two where there are only two lanes, GT = 8).
+template <int GT>
+struct RowShare {
+    static constexpr int kRows = GT == 8 ? 2 : 1;
+    uint32_t part;
+    bool any, party1;
+    __device__ __forceinline__ explicit RowShare(uint32_t lane) : part(lane % 16 / GT), any(lane % 16 / GT * kRows < 4), party1((lane & GT) != 0) {}
+    __device__ __forceinline__ uint32_t row(int x) const { return part * kRows + x; }
+    // mine: the values of this lane's party, other: those of the other one's
+    __device__ __forceinline__ Pair pick(int x, const uint64_t (&mine)[4], const uint64_t (&other)[4]) const
+    {
+        const uint32_t at = row(x);
+        const Pair y{at == 0 ? mine[0] : at == 1 ? mine[1] : at == 2 ? mine[2] : mine[3],
+                     at == 0 ? other[0] : at == 1 ? other[1] : at == 2 ? other[2] : other[3]};
+        return party1 ? Pair{y.p1, y.p0} : y;
+    }
+};
+
+// An output's sum divided by the length (the same for the whole wavefront): a truncation by its whole bits, a factor in (1/2, 1] for the rest.
+__device__ __forceinline__ Pair finish_output(const AttentionArgs &a, uint64_t i, uint32_t length, Pair sum)
+{
+    if (length == 0) return Pair{0, 0};
+    const uint64_t z = state_of(a.seed_o, 9 * i), c0 = mix64(z);
+    const int whole = 31 - __builtin_clz(length);
+    const uint64_t factor = ((1ull << (16 + whole)) + length / 2) / length;
+    const Pair o = truncate_drawn(Pair{sum.p0 + c0, sum.p1 - c0}, 16 + whole, z + kGamma);
+    return truncate_drawn(Pair{o.p0 * factor, o.p1 * factor}, 16, z + 5 * kGamma);
 }
 
 // Where a position of a sequence lies: its page, or -1 for one behind the end and for a hole.
@@ -226,49 +246,67 @@ attention_scores_kernel(AttentionArgs a)
     __shared__ unsigned long long owed[2 * GT];
     const CacheView &c = a.cache;
     const HeadChunk h = head_chunk<GT>(a, blockIdx.x);
-    const uint32_t first = blockIdx.y * a.per_scores, length = __builtin_amdgcn_readfirstlane(length_of(a, h.b));
-    const uint32_t end = first + a.per_scores < a.max_len ? first + a.per_scores : a.max_len;
+    const uint32_t threads = blockDim.x;                      // 64 for every 16 positions, up to kAttentionBlock
+    const uint32_t lane = threadIdx.x % 64, g = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint64_t row0 = (uint64_t)h.b * a.q_heads + h.first;
-    if (first >= length || c.pages == 0) {                    // all of it behind the sequence's end
-        const uint32_t count = end - first;
-        for (uint32_t i = threadIdx.x; i < h.count * count; i += kAttentionBlock) {
-            const uint64_t j = (row0 + i / count) * a.max_len + first + i % count;
+    // The queries' numbers, one a thread, in the order of their bytes in the planes: four consecutive ones are two pairs of dimensions.  A thread's first
+    // is under way before anything is waited for.
+    constexpr uint32_t kNumbers = GT * ND * 64;
+    uint64_t q0, q1;
+    auto head_of = [](uint32_t i) { return i / (ND * 64); };
+    auto dimension = [](uint32_t i) { return i / 16 % (4 * ND) * 16 + i / 4 % 4 * 2 + 8 * (i / 2 % 2) + i % 2; };
+    auto asked = [&](uint32_t i) { return head_of(i) < h.count && dimension(i) < c.dim; };
+    auto load_number = [&](uint32_t i) {
+        const uint64_t at = asked(i) ? (row0 + head_of(i)) * c.dim + dimension(i) : 0;
+        q0 = a.q[0][at];
+        q1 = a.q[1][at];
+    };
+    load_number(threadIdx.x < kNumbers ? threadIdx.x : 0);
+    const uint32_t first = blockIdx.y * a.per_scores, length = __builtin_amdgcn_readfirstlane(c.pages != 0 ? length_of(a, h.b) : 0);
+    const uint32_t end = first + a.per_scores < a.max_len ? first + a.per_scores : a.max_len;
+    auto store_zeros = [&](uint32_t from, uint32_t to, uint32_t thread, uint32_t of) {     // behind the sequence's end
+        for (uint32_t i = thread; i < h.count * (to - from); i += of) {
+            const uint64_t j = (row0 + i / (to - from)) * a.max_len + from + i % (to - from);
             a.scores[0][j] = 0;
             a.scores[1][j] = 0;
         }
-        return;
-    }
-    clear_planes<GT>(lds, kStride, owed, kAttentionBlock);
+    };
+    if (first >= length) return store_zeros(first, end, threadIdx.x, threads);
+    // The keys of 16 positions, a row each.  One without a key reads the first one's: its score is not used.
+    uint64_t there = 0, seed = 0, place = 0;
+    const uint64_t *keys = nullptr;
+    auto look_up = [&](uint32_t t0) {
+        const int64_t page = page_of(a, h.b, t0 + lane % 16, length);
+        there = __ballot(page >= 0);
+        place = page >= 0 ? place_in_page(c, h.head, (t0 + lane % 16) % c.page, 0) : 0;
+        keys = c.keys + (page >= 0 ? page : 0) * page_numbers(c) + place;
+        seed = c.page_seeds[page >= 0 ? page : 0];
+    };
+    if (first + 16 * wave < length) look_up(first + 16 * wave);
+    clear_planes<GT>(lds, kStride, owed, threads);
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < GT * ND * 16; i += kAttentionBlock) {
-        const uint32_t head = i / (ND * 16), piece = i / 4 % (4 * ND), g = i % 4;          // four dimensions: pairs of two j
-        const uint32_t d0 = 16 * piece + 2 * g;
-        uint64_t eps[4], a0[4], a1[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t d = d0 + 8 * (j / 2) + j % 2;
-            const bool there = head < h.count && d < c.dim;
-            const uint64_t at = (row0 + head) * c.dim + d;
-            const uint64_t z = state_of(a.seed_q, 2 * at);
-            a0[j] = there ? mix64(z) : 0;
-            a1[j] = there ? mix64(z + kGamma) : 0;
-            eps[j] = there ? (a.q[0][at] - a0[j]) + (a.q[1][at] - a1[j]) : 0;              // opened
-        }
-        store_vectors<GT>(lds, kStride, head, piece / 4 * 64 + 16 * g + piece % 4 * 4, eps, a0, a1, owed);
+    const QuadTurn turn(lane);
+#pragma unroll 1
+    for (uint32_t i = threadIdx.x; i < kNumbers; i += threads) {
+        if (i >= threads) load_number(i);
+        uint64_t w[2] = {state_of(a.seed_q, 2 * ((row0 + head_of(i)) * c.dim + dimension(i)))};
+        w[1] = w[0] + kGamma;
+        w[0] = asked(i) ? mix64(w[0]) : 0;
+        w[1] = asked(i) ? mix64(w[1]) : 0;
+        const uint64_t eps = asked(i) ? (q0 - w[0]) + (q1 - w[1]) : 0;                     // opened
+        store_vectors<GT>(lds, kStride, turn, i % 4, head_of(i), i / 64 % ND * 64 + i / 4 % 4 * 16 + i / 16 % 4 * 4, eps, w[0], w[1], owed);
     }
     __syncthreads();
-    const uint32_t lane = threadIdx.x % 64, g = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint8_t *column = lds + (lane % 16) * kStride + 16 * g;
     constexpr uint32_t kMatrix = Vectors<GT>::planes * kStride;
     const uint32_t chunks = (c.dim + 63) / 64;
-    for (uint32_t t0 = first + 16 * wave; t0 < end; t0 += 16 * kAttentionWaves) {
-        const uint32_t t = t0 + lane % 16;
-        const int64_t page = page_of(a, h.b, t, length);
-        const uint64_t there = __ballot(page >= 0);
-        // A row without a key reads the first one's: its score is not used.
-        const uint64_t place = page >= 0 ? place_in_page(c, h.head, t % c.page, 0) : 0;
-        const uint64_t *keys = c.keys + (page >= 0 ? page : 0) * page_numbers(c) + place;
-        uint64_t z0 = state_of(stream_word(c.page_seeds[page >= 0 ? page : 0], 0), 2 * (place + 2 * g));
+    for (uint32_t t0 = first + 16 * wave; t0 < end; t0 += threads / 4) {
+        if (t0 >= length) {
+            store_zeros(t0, t0 + 16 < end ? t0 + 16 : end, lane, 64);
+            continue;
+        }
+        if (t0 != first + 16 * wave) look_up(t0);
+        uint64_t z0 = state_of(stream_word(seed, 0), 2 * (place + 2 * g));
         i32x4_t sums[GT] = {};
         const uint8_t *at = column;
 #pragma unroll 1
@@ -294,88 +332,76 @@ attention_scores_kernel(AttentionArgs a)
         join_digits<GT>(sums, lane, owed, mine);
 #pragma unroll
         for (int r = 0; r < 4; ++r) other[r] = __shfl_xor((unsigned long long)mine[r], GT, 64);
-        // The lanes of a head share out its four rows.
-        uint32_t l = lane;
+uint32_t l = lane;
         settle(l);                                            // (nothing of this stays in registers from tile to tile)
-        const bool party1 = (l & GT) != 0;
-        const uint32_t head = l % GT, part = l % 16 / GT;
-        constexpr int kRows = GT == 8 ? 2 : 1;
-        if (part * kRows < 4 && head < h.count) {
+        const uint32_t head = l % GT;
+        const RowShare<GT> own(l);
+        if (!own.any || head >= h.count) continue;
 #pragma unroll
-            for (int x = 0; x < kRows; ++x) {
-                Pair y{mine[x], other[x]};
-#pragma unroll
-                for (int r = 1; r < 4; ++r) {
-                    if (part * kRows + x == r) y = Pair{mine[r], other[r]};
-                }
-                if (party1) y = Pair{y.p1, y.p0};
-                const uint32_t at = t0 + 4 * (l / 16) + part * kRows + x;
-                if (at >= end) continue;
-                const uint64_t j = (row0 + head) * a.max_len + at;
-                Pair score{0, 0};
-                if ((uint32_t)there >> (at - t0) & 1) {
-                    const uint64_t z = state_of(a.seed_s, 5 * j), c0 = mix64(z);
-                    score = truncate_drawn(Pair{y.p0 + c0, y.p1 - c0}, 16, z + kGamma);
-                }
-                a.scores[0][j] = score.p0;
-                a.scores[1][j] = score.p1;
+        for (int x = 0; x < RowShare<GT>::kRows; ++x) {
+            const uint32_t at = t0 + 4 * (l / 16) + own.row(x);
+            if (at >= end) continue;
+            const uint64_t j = (row0 + head) * a.max_len + at;
+            Pair score{0, 0};
+            if ((uint32_t)there >> (at - t0) & 1) {
+                const Pair y = own.pick(x, mine, other);
+                const uint64_t z = state_of(a.seed_s, 5 * j), c0 = mix64(z);
+                score = truncate_drawn(Pair{y.p0 + c0, y.p1 - c0}, 16, z + kGamma);
             }
+            a.scores[0][j] = score.p0;
+            a.scores[1][j] = score.p1;
         }
     }
 }
 
 // The product with the values.  A wavefront has 16 dimensions, the rows of its tile, and lane l takes 16 of every 64 positions; the workgroup, up to 128 dimensions,
 // makes the weights' vectors of 128 positions at a time.
-constexpr int kValueChunk = 128;
-
-template <int GT>
+template <int GT, int CHUNK>
 __global__ void __launch_bounds__(kAttentionBlock, 4)
 attention_values_kernel(AttentionArgs a)
 {
     const uint32_t threads = blockDim.x;                      // 64 for every 16 dimensions
-    constexpr uint32_t kStride = kValueChunk + 16;
+    constexpr uint32_t kStride = CHUNK + 16;
     __shared__ __align__(16) uint8_t lds[3 * Vectors<GT>::planes * kStride];
     __shared__ unsigned long long owed[2 * GT];
-    __shared__ uint64_t row_at[kValueChunk], row_state[kValueChunk];       // a position's numbers and masks
+    __shared__ uint64_t row_at[CHUNK], row_state[CHUNK];      // a position's numbers and masks
     const CacheView &c = a.cache;
     const HeadChunk h = head_chunk<GT>(a, blockIdx.x);
     const uint32_t length = __builtin_amdgcn_readfirstlane(length_of(a, h.b));
     const uint32_t first = blockIdx.y * a.per_split, end = first + a.per_split < length ? first + a.per_split : length;
-    if (first >= length) return;                              // the join does not read it
     const uint64_t row0 = (uint64_t)h.b * a.q_heads + h.first;
     const uint32_t lane = threadIdx.x % 64, g = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint32_t dim0 = blockIdx.z * (kAttentionWaves * 16) + 16 * wave, dim = dim0 + lane % 16 < c.dim ? dim0 + lane % 16 : 0;
+    if (first >= length && (length != 0 || a.splits != 1)) return;         // the join does not read it
     const uint8_t *column = lds + (lane % 16) * kStride + 16 * g;
     constexpr uint32_t kMatrix = Vectors<GT>::planes * kStride;
     clear_planes<GT>(lds, kStride, owed, threads);
     __syncthreads();
-    const uint32_t dim0 = blockIdx.z * (kAttentionWaves * 16) + 16 * wave, dim = dim0 + lane % 16 < c.dim ? dim0 + lane % 16 : 0;
     const uint64_t z = (uint64_t)(2 * dim) * kGamma;
+    const QuadTurn turn(lane);
     i32x4_t sums[GT] = {};
-    for (uint32_t t0 = first; t0 < end; t0 += kValueChunk) {
+    for (uint32_t t0 = first; t0 < end; t0 += CHUNK) {
         uint32_t thread = threadIdx.x;
         settle(thread);                                       // what follows from it is not kept in registers from chunk to chunk
-        for (uint32_t i = thread; i < kValueChunk; i += threads) {
+#pragma unroll 1
+        for (uint32_t i = thread; i < GT * CHUNK; i += threads) {
+            const uint32_t head = i / CHUNK, t = t0 + i % CHUNK;
+            const bool asked = head < h.count && t < end;
+            const uint64_t n = (row0 + (asked ? head : 0)) * a.max_len + (asked ? t : first);
+            const uint64_t p0 = a.scores[0][n], p1 = a.scores[1][n];
+            const bool there = page_of(a, h.b, t, end) >= 0 && asked;
+            const uint64_t s = state_of(a.seed_p, 2 * n), a0 = there ? mix64(s) : 0, a1 = there ? mix64(s + kGamma) : 0;
+            const uint64_t eps = there ? (p0 - a0) + (p1 - a1) : 0;                        // opened
+            store_vectors<GT>(lds, kStride, turn, i % 4, head, i % CHUNK / 4 * 4, eps, a0, a1, owed);
+        }
+        for (uint32_t i = thread; i < CHUNK; i += threads) {
             const int64_t page = page_of(a, h.b, t0 + i, end);
             const uint64_t place = place_in_page(c, h.head, (t0 + i) % c.page, 0);
             row_at[i] = page >= 0 ? page * page_numbers(c) + place : 0;       // without a value: the first one's, times zeros
             row_state[i] = page >= 0 ? state_of(stream_word(c.page_seeds[page], 1), 2 * place) : 0;
         }
-        for (uint32_t i = thread; i < GT * kValueChunk / 4; i += threads) {
-            const uint32_t head = i / (kValueChunk / 4), at = i % (kValueChunk / 4) * 4;
-            uint64_t eps[4], a0[4], a1[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t t = t0 + at + j;
-                const bool there = head < h.count && page_of(a, h.b, t, end) >= 0;
-                const uint64_t n = (row0 + head) * a.max_len + t, z = state_of(a.seed_p, 2 * n);
-                a0[j] = there ? mix64(z) : 0;
-                a1[j] = there ? mix64(z + kGamma) : 0;
-                eps[j] = there ? (a.scores[0][n] - a0[j]) + (a.scores[1][n] - a1[j]) : 0;  // opened
-            }
-            store_vectors<GT>(lds, kStride, head, at, eps, a0, a1, owed);
-        }
         __syncthreads();
-        for (uint32_t block = 0; block < kValueChunk / 64 && t0 + 64 * block < end && c.pages != 0; ++block) {
+        for (uint32_t block = 0; block < CHUNK / 64 && t0 + 64 * block < end && c.pages != 0; ++block) {
 auto numbers = [&](uint64_t (&delta)[16]) {
 #pragma unroll
                 for (int j = 0; j < 16; ++j) delta[j] = load_stream(c.values + row_at[64 * block + 16 * g + j] + dim);
@@ -387,23 +413,41 @@ auto numbers = [&](uint64_t (&delta)[16]) {
         }
         __syncthreads();
     }
-    // One partial sum for each number of the output and party, in lanes of the first half of a tile's columns that hold it.
+    // Of each number and party one partial sum, or the result where there is one split.
     const uint64_t numbers = (uint64_t)a.batch * a.q_heads * c.dim;
-    uint32_t column_of = lane;
-    settle(column_of);
-    const uint32_t head = column_of % GT;
-    const uint64_t party = (column_of & GT) != 0;
-uint64_t y[4];
+    uint32_t l = lane;
+    settle(l);
+    const uint32_t head = l % GT;
+    const bool party1 = (l & GT) != 0;
+    uint64_t y[4];
     join_digits<GT>(sums, lane, owed, y);
-    if (lane % 16 >= Vectors<GT>::nv || head >= h.count) return;
+    if (a.splits != 1) {
+        if (l % 16 >= Vectors<GT>::nv || head >= h.count) return;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const uint32_t to = dim0 + 4 * g + r;
-        if (to < c.dim) a.parts[(2 * (uint64_t)blockIdx.y + party) * numbers + (row0 + head) * c.dim + to] = y[r];
+        for (int r = 0; r < 4; ++r) {
+            const uint32_t to = dim0 + 4 * (l / 16) + r;
+            if (to < c.dim) a.parts[(2 * (uint64_t)blockIdx.y + party1) * numbers + (row0 + head) * c.dim + to] = y[r];
+        }
+        return;
+    }
+    uint64_t other[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) other[r] = __shfl_xor((unsigned long long)y[r], GT, 64);
+    const RowShare<GT> mine(l);
+    if (!mine.any || head >= h.count) return;
+#pragma unroll
+    for (int x = 0; x < RowShare<GT>::kRows; ++x) {
+        const Pair sum = mine.pick(x, y, other);
+        const uint32_t to = dim0 + 4 * (l / 16) + mine.row(x);
+        if (to >= c.dim) continue;
+        const uint64_t i = (row0 + head) * c.dim + to;
+        const Pair o = finish_output(a, i, length, sum);
+        a.out[0][i] = o.p0;
+        a.out[1][i] = o.p1;
     }
 }
 
-// Joins the splits and divides by the length: a truncation by its whole bits, a factor in (1/2, 1] for the rest.  32 numbers a workgroup, whose
+// Joins the splits and divides by the length.  32 numbers a workgroup, whose
 // splits eight threads each share out.
 constexpr int kJoinNumbers = 32, kJoinShares = kJoinBlock / kJoinNumbers;
 
@@ -427,19 +471,13 @@ attention_join_kernel(AttentionArgs a)
     partial[1][share][x] = o.p1;
     __syncthreads();
     if (share != 0 || at >= per) return;
-    if (length != 0) {
-        const uint64_t z = state_of(a.seed_o, 9 * i), c0 = mix64(z);
-        o = Pair{c0, 0 - c0};
+    o = Pair{0, 0};
 #pragma unroll
-        for (int s = 0; s < kJoinShares; ++s) {
-            o.p0 += partial[0][s][x];
-            o.p1 += partial[1][s][x];
-        }
-        const int whole = 31 - __builtin_clz(length);
-        const uint64_t factor = ((1ull << (16 + whole)) + length / 2) / length;
-        o = truncate_drawn(o, 16 + whole, z + kGamma);
-        o = truncate_drawn(Pair{o.p0 * factor, o.p1 * factor}, 16, z + 5 * kGamma);
+    for (int s = 0; s < kJoinShares; ++s) {
+        o.p0 += partial[0][s][x];
+        o.p1 += partial[1][s][x];
     }
+    o = finish_output(a, i, length, o);
     a.out[0][i] = o.p0;
     a.out[1][i] = o.p1;
 }

@@ -92,6 +92,30 @@ __device__ __forceinline__ void digits_of(const uint64_t (&v)[4], uint32_t (&out
     for (int i = 0; i < 8; ++i) out[i] ^= kDigitFlip;
 }
 
+// The same turn of bytes across four neighbouring lanes, of a word each: the word of lane j (mod 4) becomes byte j of the four.  All four lanes run.
+struct QuadTurn {
+    uint32_t first, second;     // this lane's byte selectors
+    __device__ __forceinline__ explicit QuadTurn(uint32_t lane)
+        : first(lane & 1 ? 0x03070105u : 0x06020400u), second(lane & 2 ? 0x03020706u : 0x05040100u) {}
+    __device__ __forceinline__ uint32_t operator()(uint32_t w) const
+    {
+        const uint32_t next = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w, 0xB1, 0xF, 0xF, true);       // of lane ^ 1
+        w = __builtin_amdgcn_perm(next, w, first);
+        const uint32_t far = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w, 0x4E, 0xF, 0xF, true);        // of lane ^ 2
+        return __builtin_amdgcn_perm(far, w, second);
+    }
+};
+// Sum over four neighbouring lanes, in all of them.
+__device__ __forceinline__ uint64_t quad_sum(uint64_t v)
+{
+    const uint32_t l1 = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, 0xB1, 0xF, 0xF, true);
+    const uint32_t h1 = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), 0xB1, 0xF, 0xF, true);
+    v += (uint64_t)h1 << 32 | l1;
+    const uint32_t l2 = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, 0x4E, 0xF, 0xF, true);
+    const uint32_t h2 = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), 0x4E, 0xF, 0xF, true);
+    return v + ((uint64_t)h2 << 32 | l2);
+}
+
 // c + A B of 16 x 64 by 64 x 16 int8.  Lane l holds 16 numbers of row (A) or column (B) l mod 16 in each of its four registers' bytes, those of
 // the same 16 places of the sum in A and B (lanes l with the same l / 16 share them); which places is the caller's choice.  The result's lane l
 // holds rows 4 (l / 16) .. + 3 of column l mod 16.
