@@ -5,9 +5,6 @@
 
 #include <type_traits>
 
-#ifndef VC
-#define VC 0
-#endif
 namespace {
 
 // What a cache has to be, whatever is done with it.
@@ -79,9 +76,15 @@ AttentionLayout attention_layout(const hb_cache *cache, size_t batch, int q_head
 {
     AttentionLayout lay = {};
     const size_t scores = round_up(8 * batch * q_heads * max_len), numbers = batch * q_heads * cache->dim;
-    // Positions of a workgroup: what gives every compute unit two workgroups at a time, four where lengths may differ.
+    // Positions of a workgroup: what gives every compute unit two workgroups at a time, four where lengths may differ (eight sequences of none to
+    // 4096 145 us, with two 155; 32768 positions of one 183, with four 194, with one 205); no fewer than make the vectors of a workgroup's heads,
+    // which are the same for 16 positions and for 1000, worth their time (eight heads, 2048 positions of four sequences 48 us with 128 at least, 73 with
+    // 32; 1000 of one 33 with 64, 40 with 128, 63 with 256).
     const size_t some = batch != 0 ? batch : 1, groups = some * cache->heads * head_chunks(cache, q_heads), pieces = ((batch > 1 ? 1024 : 512) + groups - 1) / groups;
+    const int together = heads_together(cache, q_heads);
+    const size_t least = together < 8 ? 16 * together : groups * ((max_len + 63) / 64) <= 256 ? 64 : 128;
     size_t per = (max_len + pieces - 1) / pieces;
+    if (per < least) per = least;
     per = per > 64 ? (per + 127) / 128 * 128 : per > 32 ? 64 : per > 16 ? 32 : 16;
     if (per > hb::kMostPlaces) per = hb::kMostPlaces;
     lay.per_scores = (uint32_t)per;
@@ -127,7 +130,7 @@ void launch_values(const hb::AttentionArgs &a, int together, dim3 grid, hipStrea
     const dim3 block(64 * (grid.z > 1 ? most : tiles));
     with_heads(together, [&](auto heads) {
         constexpr int GT = decltype(heads)::value;
-        if (GT == 8 || a.per_split <= 64 || VC) hipLaunchKernelGGL((hb::attention_values_kernel<GT, 64>), grid, block, 0, stream, a);
+        if (GT == 8 || a.per_split <= 64) hipLaunchKernelGGL((hb::attention_values_kernel<GT, 64>), grid, block, 0, stream, a);
         else hipLaunchKernelGGL((hb::attention_values_kernel<GT, GT == 8 ? 64 : 128>), grid, block, 0, stream, a);
     });
 }
