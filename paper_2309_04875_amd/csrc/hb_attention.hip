@@ -57,7 +57,7 @@ struct AttentionLayout {
 bool attention_sizes(const hb_cache *cache, size_t batch, int q_heads, size_t max_len)
 {
     return check_cache(cache) == HB_OK && q_heads >= cache->heads && q_heads <= 65536 && q_heads % cache->heads == 0 && batch <= 65535 &&
-           max_len <= ((size_t)1 << 29) && batch * q_heads * max_len <= HB_MAX_ELEMENTS;
+           max_len <= HB_ATTENTION_MAX_LEN && batch * q_heads * max_len <= HB_MAX_ELEMENTS;
 }
 
 // Query heads that a workgroup takes together, a power of two up to eight, and how many such chunks a head of the cache has.

@@ -37,11 +37,12 @@ constexpr int kAttentionBlock = 512, kAttentionWaves = kAttentionBlock / 64, kJo
 // rows a tile; the right operand of matrix digit i has a column (s, v) for every weight 2^(8s) and vector v = party * GT + head that holds digit s - i
 // of v, nothing where s < i: 16 GT columns, GT tiles.  The vectors' digits lie in LDS as planes [digit][v], the columns of digit i
 // are the planes 2 GT i further up, and planes of zeros lie before the first; a tile whose columns all have s < i is left out (36 of 64
-// products at GT = 8, 20 of 32 at GT = 4).  int32 sums hold 2^17 a place: 2^14 places at most go into one.
+// products at GT = 8, 20 of 32 at GT = 4).  int32 sums hold up to 8 x 2^14 a place and matrix: 2^12 places at most go into one.
 //
 // The matrices' words go in with their bytes' top bits flipped, which is a number less 0x80..80: every vector's result is owed that constant times the sum of
 // its entries over the three matrices (owed[v]).
-constexpr int kZeroPlanes = 16, kMostPlaces = 1 << 14;
+constexpr int kZeroPlanes = 16, kMostPlaces = 1 << 12;
+static_assert(3ll * 8 * 128 * 128 * kMostPlaces < 1ll << 31, "sums of digit products");
 
 template <int GT>
 struct Vectors {

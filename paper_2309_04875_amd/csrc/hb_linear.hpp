@@ -13,10 +13,11 @@ struct LinearArgs {
     uint64_t seedA, weight_bytes;
     uint64_t group_inverse;     // ceil(2^40 / group): input / group is (input * group_inverse) >> 40
     uint32_t rows, in, outs, groups;
-    uint32_t row_tiles, out_tiles;
+    uint32_t row_tiles;
     int frac;
 };
 
+constexpr uint32_t kDies = 8;
 constexpr int kLinearStep = 256;                     // inputs of a step
 constexpr int kLinearPlane = kLinearStep + 16;       // bytes of a digit's plane in LDS: rows of it fall into different banks
 
@@ -137,7 +138,10 @@ linear_q4_kernel(LinearArgs a)
     __shared__ __align__(16) uint8_t lds[kBuffers * kBlockBytes];
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint32_t q = lane / 16, wn = wave % WN, wk = wave / WN;
-    const uint32_t row0 = (blockIdx.x % a.row_tiles) * TM, tile0 = (blockIdx.x / a.row_tiles) * (WN * RT) + wn * RT;
+    // Workgroups with the same weights run on the same die (they are dealt out to the eight in turn), whose cache then reads them once.
+    const uint32_t place = blockIdx.x / kDies, group0 = place / a.row_tiles * kDies + blockIdx.x % kDies;
+    const uint32_t row0 = place % a.row_tiles * TM, tile0 = group0 * (WN * RT) + wn * RT;
+    if (16 * group0 * (WN * RT) >= a.outs) return;
     const uint32_t steps = (a.in + kLinearStep - 1) / kLinearStep;
     // A lane's rows of weights and scales; outputs behind the last are the last.
     const uint8_t *weight_row[RT];
@@ -276,7 +280,7 @@ linear_q4_kernel(LinearArgs a)
     }
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < kSums / 2; i += 64 * WN * WK) {
-        const uint32_t m = i / (RT * WN * 16), tile = (blockIdx.x / a.row_tiles) * (WN * RT) + i / 16 % (RT * WN);
+        const uint32_t m = i / (RT * WN * 16), tile = group0 * (WN * RT) + i / 16 % (RT * WN);
         const uint32_t row = row0 + m, out = 16 * tile + i % 16;
         if (row >= a.rows || out >= a.outs) continue;
         const uint64_t at = (uint64_t)row * a.outs + out;

@@ -23,7 +23,7 @@ def test_workspace_sizes():
     assert _workspace(0, 2, 100) == _workspace(0, 2, 0) == 0                     # of nothing
     sizes = [_workspace(3, 4, n) for n in (0, 1, 63, 64, 65, 1000, 100000, 1 << 25)]
     assert sizes == sorted(sizes) and all(s % 256 == 0 for s in sizes)
-    for bad in ((1, 3, 10), (1, 1, 10), (1, 0, 10), (1, -2, 10), (65536, 2, 10), (1, 2, (1 << 29) + 1), (60000, 2, 1 << 28)):
+    for bad in ((1, 3, 10), (1, 1, 10), (1, 0, 10), (1, -2, 10), (65536, 2, 10), (1, 2, (1 << 27) + 1), (60000, 4, 1 << 26)):
         assert _workspace(*bad) == 0, bad
     for cache in (dict(dim=15), dict(dim=0), dict(dim=258), dict(heads=0), dict(page=0), dict(page=65537), dict(pages=1 << 31), dict(pages=1 << 30, page=65536, dim=256)):
         assert _workspace(1, 2, 10, **cache) == 0, cache
