@@ -130,8 +130,8 @@ void launch_values(const hb::AttentionArgs &a, int together, dim3 grid, hipStrea
     const dim3 block(64 * (grid.z > 1 ? most : tiles));
     with_heads(together, [&](auto heads) {
         constexpr int GT = decltype(heads)::value;
-        if (GT == 8 || a.per_split <= 64) hipLaunchKernelGGL((hb::attention_values_kernel<GT, 64>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((hb::attention_values_kernel<GT, GT == 8 ? 64 : 128>), grid, block, 0, stream, a);
+        if (GT >= 4 || a.per_split <= 64) hipLaunchKernelGGL((hb::attention_values_kernel<GT, 64>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((hb::attention_values_kernel<GT, GT >= 4 ? 64 : 128>), grid, block, 0, stream, a);
     });
 }
 

@@ -34,146 +34,175 @@ constexpr int kAttentionBlock = 512, kAttentionWaves = kAttentionBlock / 64, kJo
 // so three matrices, b_0, b_1 and D, meet two vectors for each query head, one for each party: b_0 {eps, a}, b_1 {0, a + eps}, D {eps + a_0, a_1}.
 //
 // In digits: sum over s of 2^(8s) of sum over i <= s of (digit i of the matrix) (digit s - i of the vectors).  Matrices are the left operands, 16
-// rows a tile; the right operand of matrix digit i has a column (s, v) for every weight 2^(8s) and vector v = party * GT + head that holds digit s - i
-// of v, nothing where s < i: 16 GT columns, GT tiles.  The vectors' digits lie in LDS as planes [digit][v], the columns of digit i
-// are the planes 2 GT i further up, and planes of zeros lie before the first; a tile whose columns all have s < i is left out (36 of 64
-// products at GT = 8, 20 of 32 at GT = 4).  int32 sums hold up to 8 x 2^14 a place and matrix: 2^12 places at most go into one.
+// rows a tile; the right operand has a column (s, v) for every weight 2^(8s) and vector v = party * GT + head: 16 GT columns, GT tiles.  int32 sums
+// hold up to 8 x 2^14 a place and matrix: 2^12 places at most go into one.
 //
 // The matrices' words go in with their bytes' top bits flipped, which is a number less 0x80..80: every vector's result is owed that constant times the sum of
 // its entries over the three matrices (owed[v]).
-constexpr int kZeroPlanes = 16, kMostPlaces = 1 << 12;
+//
+// Two forms.  WHOLE: a left operand is the lower (or upper) halves of four numbers as they are, four digits each, and a column holds for a number the
+// digits s, s-1, s-2, s-3 of its vector (for the upper halves s-4 ..: the columns of weight 2^(8(s-4))), zeros below digit 0: planes [s][v] of four
+// bytes a place.  Otherwise digit i of 16 numbers is an operand, their bytes turned before (12 instructions a number of the cache and its two
+// masks, of 61), and a column holds digit s - i: planes [digit][v] of a byte a place, the columns of digit i being the planes 2 GT i further up,
+// planes of zeros before the first, and tiles whose columns all have s < i left out.  WHOLE has fewer instructions, but four times the planes to
+// write and to hold: it is for one or two heads at a time (32 heads of 4096 positions of 128, one query head each, 85 -> 78 us; 8192 of 8 heads 53 -> 49; eight
+// sequences of none to 4096 with two 126 -> 117) and, 64 positions at a time, for the values of four (2 x 4096 of 192 110 -> 104, 4 x 1000 of 128 40 -> 39; their
+// scores stay as they were, or with few positions lose: 39 -> 46).
+constexpr int kMostPlaces = 1 << 12;
 static_assert(3ll * 8 * 128 * 128 * kMostPlaces < 1ll << 31, "sums of digit products");
 
-template <int GT>
-struct Vectors {
-    static constexpr int nv = 2 * GT, planes = kZeroPlanes + 8 * nv;          // planes of one matrix
-    static constexpr bool used(int i, int tile) { return i * nv <= 16 * tile + 15; }
-};
+template <int GT, bool WHOLE, int PLACES>
+struct Planes {
+    static constexpr int nv = 2 * GT, zeros = WHOLE ? (GT == 1 ? 8 : 0) : 16, rows = zeros + 8 * nv;          // of one matrix
+    static constexpr uint32_t stride = (WHOLE ? 4 : 1) * PLACES + 16;         // (16 more: rows of 16 fall into different banks)
+    static constexpr uint32_t matrix = rows * stride, bytes = 3 * matrix;
+    // A lane's part of the columns: of every 64 places lane quarter g has 16 g .. 16 g + 15.
+    static constexpr uint32_t per_64 = WHOLE ? 256 : 64;
+    static __device__ __forceinline__ const uint8_t *column(const uint8_t *lds, uint32_t lane) { return lds + lane % 16 * stride + lane / 16 * (per_64 / 4); }
 
-// Digits of one place of vector v, four lanes side by side having four consecutive places, the first at byte `at` of its planes: a lane writes digits j
-// and 4 + j of all four, j = lane mod 4.
-template <int GT>
-__device__ __forceinline__ void store_vector(uint8_t *planes, uint32_t stride, const QuadTurn &turn, uint32_t j, uint32_t v, uint32_t at, uint64_t x)
-{
-    x += kDigitBias;
-    uint8_t *to = planes + (kZeroPlanes + j * Vectors<GT>::nv + v) * stride + at;
-    *reinterpret_cast<uint32_t *>(to) = turn((uint32_t)x) ^ kDigitFlip;
-    *reinterpret_cast<uint32_t *>(to + 4 * Vectors<GT>::nv * stride) = turn((uint32_t)(x >> 32)) ^ kDigitFlip;
-}
-
-// The vectors of one query head for the three matrices, a place a lane; what is not there is zeros.
-template <int GT>
-__device__ __forceinline__ void store_vectors(uint8_t *lds, uint32_t stride, const QuadTurn &turn, uint32_t j, uint32_t head, uint32_t at, uint64_t eps,
-                                              uint64_t a0, uint64_t a1, unsigned long long *owed)
-{
-    const uint32_t matrix = Vectors<GT>::planes * stride;
-    store_vector<GT>(lds, stride, turn, j, head, at, eps);
-    store_vector<GT>(lds, stride, turn, j, GT + head, at, a0 + a1);
-    store_vector<GT>(lds + matrix, stride, turn, j, GT + head, at, a0 + a1 + eps);
-    store_vector<GT>(lds + 2 * matrix, stride, turn, j, head, at, eps + a0);
-    store_vector<GT>(lds + 2 * matrix, stride, turn, j, GT + head, at, a1);
-    const uint64_t owed0 = quad_sum(2 * eps + a0), owed1 = quad_sum(2 * a0 + 3 * a1 + eps);
-    if (j < 2) atomicAdd(&owed[j * GT + head], (unsigned long long)(kDigitBias * (j == 0 ? owed0 : owed1)));
-}
-
-// Zeros where no vector is: before the planes, and party 0's vectors for b_1.
-template <int GT>
-__device__ __forceinline__ void clear_planes(uint8_t *lds, uint32_t stride, unsigned long long *owed, uint32_t threads)
-{
-    if (threadIdx.x < 2 * GT) owed[threadIdx.x] = 0;
-    const uint32_t matrix = Vectors<GT>::planes * stride, words = stride / 4;
-    for (uint32_t i = threadIdx.x; i < 3 * kZeroPlanes * words; i += threads)
-        *reinterpret_cast<uint32_t *>(lds + i / (kZeroPlanes * words) * matrix + i % (kZeroPlanes * words) * 4) = 0;
-    for (uint32_t i = threadIdx.x; i < 8 * GT * words; i += threads) {
-        const uint32_t plane = i / words;
-        *reinterpret_cast<uint32_t *>(lds + matrix + (kZeroPlanes + plane / GT * Vectors<GT>::nv + plane % GT) * stride + i % words * 4) = 0;
-    }
-}
-
-typedef uint32_t MatrixDigits[8][4];      // a lane's 16 numbers of a row: digit, four numbers a word
-
-// sums += digits times one matrix's vectors; column: this lane's first plane (lane mod 16) at its places.
-template <int GT>
-__device__ __forceinline__ void multiply(i32x4_t (&sums)[GT], const MatrixDigits &d, const uint8_t *column, uint32_t stride)
-{
+    // Place i of vector v.  Four lanes side by side have places 4 n .. 4 n + 3.
+    static __device__ __forceinline__ void store(uint8_t *planes, const QuadTurn &turn, uint32_t i, uint32_t v, uint64_t x)
+    {
+        x += kDigitBias;
+        if constexpr (WHOLE) {
+            // the digits from the highest on: bytes 7 - s .. 10 - s of these eight and zeros
+            const uint32_t high = __builtin_bswap32((uint32_t)(x >> 32) ^ kDigitFlip), low = __builtin_bswap32((uint32_t)x ^ kDigitFlip);
+            uint8_t *to = planes + (zeros + v) * stride + 4 * i;
+            const uint32_t w[8] = {low >> 24, low >> 16, low >> 8, low, __builtin_amdgcn_alignbyte(low, high, 3), __builtin_amdgcn_alignbyte(low, high, 2),
+                                   __builtin_amdgcn_alignbyte(low, high, 1), high};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const i32x4_t left{(int)d[i][0], (int)d[i][1], (int)d[i][2], (int)d[i][3]};
-#pragma unroll
-        for (int tile = 0; tile < GT; ++tile) {
-            if (!Vectors<GT>::used(i, tile)) continue;
-            const i32x4_t right = *reinterpret_cast<const i32x4_t *>(column + (kZeroPlanes + 16 * tile - i * Vectors<GT>::nv) * stride);
-            sums[tile] = mfma_16x16x64(left, right, sums[tile]);
+            for (int s = 0; s < 8; ++s) *reinterpret_cast<uint32_t *>(to + s * nv * stride) = w[s];
+        } else {
+            const uint32_t j = i % 4;                         // this lane writes digits j and 4 + j of all four
+            uint8_t *to = planes + (zeros + j * nv + v) * stride + i - j;
+            *reinterpret_cast<uint32_t *>(to) = turn((uint32_t)x) ^ kDigitFlip;
+            *reinterpret_cast<uint32_t *>(to + 4 * nv * stride) = turn((uint32_t)(x >> 32)) ^ kDigitFlip;
         }
     }
-}
 
-__device__ __forceinline__ void digits_at(MatrixDigits &d, int s, const uint64_t (&v)[4])
-{
-    uint32_t w[8];
-    digits_of_flipped(v, w);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) d[i][s] = w[i];
-}
-
-// Digits of 16 dealer words, state(j) that of word j, eight in step (four: 1 to 4 % slower; 16: as fast).
-template <class State>
-__device__ __forceinline__ void draw_digits(MatrixDigits &d, const State &state)
-{
-    constexpr int IN_STEP = 8;
-#pragma unroll
-    for (int s = 0; s < 4; s += IN_STEP / 4) {
-        uint64_t z[IN_STEP];
-#pragma unroll
-        for (int j = 0; j < IN_STEP; ++j) z[j] = state(4 * s + j);
-        mix_flipped<true>(z);
-#pragma unroll
-        for (int x = 0; x < IN_STEP / 4; ++x) digits_at(d, s + x, {z[4 * x], z[4 * x + 1], z[4 * x + 2], z[4 * x + 3]});
+    // The vectors of one query head for the three matrices, place i; what is not there is zeros.
+    static __device__ __forceinline__ void store_vectors(uint8_t *lds, const QuadTurn &turn, uint32_t i, uint32_t head, uint64_t eps, uint64_t a0, uint64_t a1,
+                                                         unsigned long long *owed)
+    {
+        store(lds, turn, i, head, eps);
+        store(lds, turn, i, GT + head, a0 + a1);
+        store(lds + matrix, turn, i, GT + head, a0 + a1 + eps);
+        store(lds + 2 * matrix, turn, i, head, eps + a0);
+        store(lds + 2 * matrix, turn, i, GT + head, a1);
+        const uint64_t owed0 = quad_sum(2 * eps + a0), owed1 = quad_sum(2 * a0 + 3 * a1 + eps);
+        if (i % 4 < 2) atomicAdd(&owed[i % 4 * GT + head], (unsigned long long)(kDigitBias * (i % 4 == 0 ? owed0 : owed1)));
     }
-}
-__device__ __forceinline__ void masked_digits(MatrixDigits &d, const uint64_t (&delta)[16])
-{
-#pragma unroll
-    for (int s = 0; s < 4; ++s)
-        digits_at(d, s, {delta[4 * s] ^ kDigitBias, delta[4 * s + 1] ^ kDigitBias, delta[4 * s + 2] ^ kDigitBias, delta[4 * s + 3] ^ kDigitBias});
-}
 
-// sums += the three matrices, 16 numbers a lane each, times their vectors: numbers(x) loads D, words(p, d) draws the digits of b_p.
-// EARLY: the loads are under way while words are drawn.  That holds 32 registers more: where they are there (128 for four wavefronts a SIMD)
-// it is 10 to 20 % faster (scores of 1111 positions at dim 80 24 us instead of 31), where they are not, spills cost more (values with
-// GT = 4, 32768 positions 115 instead of 96).
-template <int GT, bool EARLY, class Numbers, class Words>
-__device__ __forceinline__ void multiply_three(i32x4_t (&sums)[GT], const uint8_t *column, uint32_t matrix, uint32_t stride, const Numbers &numbers,
-                                               const Words &words)
-{
-    uint64_t delta[16];
-    MatrixDigits d;
-    auto masked = [&] {
-        masked_digits(d, delta);
-        multiply<GT>(sums, d, column + 2 * matrix, stride);
-    };
-    numbers(delta);
-    if constexpr (!EARLY) {
-        masked();
-        __builtin_amdgcn_sched_barrier(0);                    // D leaves its registers before words are drawn
+    // Zeros where no vector is: before the planes, and party 0's vectors for b_1.
+    static __device__ __forceinline__ void clear(uint8_t *lds, unsigned long long *owed, uint32_t threads)
+    {
+        if (threadIdx.x < nv) owed[threadIdx.x] = 0;
+        constexpr uint32_t words = stride / 4;
+        if constexpr (zeros != 0) {
+            for (uint32_t i = threadIdx.x; i < 3 * zeros * words; i += threads)
+                *reinterpret_cast<uint32_t *>(lds + i / (zeros * words) * matrix + i % (zeros * words) * 4) = 0;
+        }
+        for (uint32_t i = threadIdx.x; i < 8 * GT * words; i += threads) {
+            const uint32_t plane = i / words;
+            *reinterpret_cast<uint32_t *>(lds + matrix + (zeros + plane / GT * nv + plane % GT) * stride + i % words * 4) = 0;
+        }
     }
+
+    typedef uint32_t Digits[8][4];            // otherwise: a lane's 16 numbers of a row: digit, four numbers a word
+
+    static __device__ __forceinline__ i32x4_t operand(const uint8_t *at) { return *reinterpret_cast<const i32x4_t *>(at); }
+    // sums += numbers 4 s .. 4 s + 3 (bytes flipped) of one matrix times its vectors.
+    static __device__ __forceinline__ void multiply(i32x4_t (&sums)[GT], uint64_t z0, uint64_t z1, uint64_t z2, uint64_t z3, int s, const uint8_t *column)
+    {
+        const i32x4_t low{(int)z0, (int)z1, (int)z2, (int)z3}, high{(int)(z0 >> 32), (int)(z1 >> 32), (int)(z2 >> 32), (int)(z3 >> 32)};
+        i32x4_t right[GT];
+#pragma unroll
+        for (int tile = 0; tile < GT; ++tile) {
+            right[tile] = operand(column + (zeros + 16 * tile) * stride + 16 * s);
+            sums[tile] = mfma_16x16x64(low, right[tile], sums[tile]);
+        }
+        // the upper halves meet the columns of four weights less
+        if constexpr (GT == 1) {
+            sums[0] = mfma_16x16x64(high, operand(column + 16 * s), sums[0]);
+        } else {
+#pragma unroll
+            for (int tile = GT / 2; tile < GT; ++tile) sums[tile] = mfma_16x16x64(high, right[tile - GT / 2], sums[tile]);
+        }
+    }
+    // The same of digits of all 16.
+    static __device__ __forceinline__ void multiply(i32x4_t (&sums)[GT], const Digits &d, const uint8_t *column)
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const i32x4_t left{(int)d[i][0], (int)d[i][1], (int)d[i][2], (int)d[i][3]};
+#pragma unroll
+            for (int tile = 0; tile < GT; ++tile) {
+                if (i * nv > 16 * tile + 15) continue;
+                sums[tile] = mfma_16x16x64(left, operand(column + (zeros + 16 * tile - i * nv) * stride), sums[tile]);
+            }
+        }
+    }
+    static __device__ __forceinline__ void digits_at(Digits &d, int s, uint64_t z0, uint64_t z1, uint64_t z2, uint64_t z3)
+    {
+        uint32_t w[8];
+        digits_of_flipped({z0, z1, z2, z3}, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i][s] = w[i];
+    }
+
+    // sums += the three matrices, 16 numbers a lane each, times their vectors: numbers(x) loads D, state(p, j) is that of the word for number j of b_p.
+    // Words are drawn eight in step (four: 1 to 4 % slower; 16: as fast).  The loads are under way while words are drawn, but for GT = 8, where the
+    // 32 registers that they hold would be the fifth wavefront's on a SIMD.
+    template <class Numbers, class State>
+    static __device__ __forceinline__ void multiply_three(i32x4_t (&sums)[GT], const uint8_t *column, const Numbers &numbers, const State &state)
+    {
+        uint64_t delta[16];
+        Digits d;
+        auto masked = [&] {
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                uint64_t z[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) z[j] = delta[4 * s + j] ^ kDigitBias;
+                if constexpr (WHOLE) multiply(sums, z[0], z[1], z[2], z[3], s, column + 2 * matrix);
+                else digits_at(d, s, z[0], z[1], z[2], z[3]);
+            }
+            if constexpr (!WHOLE) multiply(sums, d, column + 2 * matrix);
+        };
+        numbers(delta);
+        if constexpr (GT == 8) {
+            masked();
+            __builtin_amdgcn_sched_barrier(0);                // D leaves its registers before words are drawn
+        }
 #pragma unroll 1
-    for (int p = 0; p < 2; ++p) {
-        words(p, d);
-        multiply<GT>(sums, d, column + p * matrix, stride);
+        for (int p = 0; p < 2; ++p) {
+#pragma unroll
+            for (int s = 0; s < 4; s += 2) {
+                uint64_t z[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) z[j] = state(p, 4 * s + j);
+                mix_flipped<true>(z);
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    if constexpr (WHOLE) multiply(sums, z[4 * x], z[4 * x + 1], z[4 * x + 2], z[4 * x + 3], s + x, column + p * matrix);
+                    else digits_at(d, s + x, z[4 * x], z[4 * x + 1], z[4 * x + 2], z[4 * x + 3]);
+                }
+            }
+            if constexpr (!WHOLE) multiply(sums, d, column + p * matrix);
+        }
+        if constexpr (GT != 8) masked();
     }
-    if constexpr (EARLY) masked();
-}
+};
 
 // The weights 2^(8s) put together: value[r] of vector v = lane mod 2 GT and row 4 (lane / 16) + r, in all lanes with that v.
 template <int GT>
 __device__ __forceinline__ void join_digits(const i32x4_t (&sums)[GT], uint32_t lane, const unsigned long long *owed, uint64_t (&value)[4])
 {
-    constexpr int kPer = 16 / Vectors<GT>::nv;                 // values of s in a tile
+    constexpr int kPer = 16 / (2 * GT);                 // values of s in a tile
     // 2^(8 s') of this lane's s' = s mod kPer
     uint64_t weight = 1;
 #pragma unroll
-    for (int s = 1; s < kPer; ++s) weight = lane % 16 / Vectors<GT>::nv == s ? 1ull << (8 * s) : weight;
+    for (int s = 1; s < kPer; ++s) weight = lane % 16 / (2 * GT) == s ? 1ull << (8 * s) : weight;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         uint64_t y = 0;
@@ -181,8 +210,8 @@ __device__ __forceinline__ void join_digits(const i32x4_t (&sums)[GT], uint32_t 
         for (int tile = 0; tile < GT; ++tile) y += (uint64_t)(int64_t)sums[tile][r] << (8 * kPer * tile);
         if constexpr (kPer > 1) y *= weight;
 #pragma unroll
-        for (int step = Vectors<GT>::nv; step < 16; step *= 2) y += __shfl_xor((unsigned long long)y, step, 64);
-        value[r] = y + owed[lane % Vectors<GT>::nv];
+        for (int step = (2 * GT); step < 16; step *= 2) y += __shfl_xor((unsigned long long)y, step, 64);
+        value[r] = y + owed[lane % (2 * GT)];
     }
 }
 
@@ -242,8 +271,8 @@ template <int GT, int ND>
 __global__ void __launch_bounds__(kAttentionBlock, 4)
 attention_scores_kernel(AttentionArgs a)
 {
-    constexpr uint32_t kStride = 64 * ND + 16;
-    __shared__ __align__(16) uint8_t lds[3 * Vectors<GT>::planes * kStride];
+    using P = Planes<GT, (GT <= 2 && GT * ND < 8), 64 * ND>;     // two workgroups' on a compute unit
+    __shared__ __align__(16) uint8_t lds[P::bytes];
     __shared__ unsigned long long owed[2 * GT];
     const CacheView &c = a.cache;
     const HeadChunk h = head_chunk<GT>(a, blockIdx.x);
@@ -284,7 +313,7 @@ attention_scores_kernel(AttentionArgs a)
         seed = c.page_seeds[page >= 0 ? page : 0];
     };
     if (first + 16 * wave < length) look_up(first + 16 * wave);
-    clear_planes<GT>(lds, kStride, owed, threads);
+    P::clear(lds, owed, threads);
     __syncthreads();
     const QuadTurn turn(lane);
 #pragma unroll 1
@@ -295,11 +324,10 @@ attention_scores_kernel(AttentionArgs a)
         w[0] = asked(i) ? mix64(w[0]) : 0;
         w[1] = asked(i) ? mix64(w[1]) : 0;
         const uint64_t eps = asked(i) ? (q0 - w[0]) + (q1 - w[1]) : 0;                     // opened
-        store_vectors<GT>(lds, kStride, turn, i % 4, head_of(i), i / 64 % ND * 64 + i / 4 % 4 * 16 + i / 16 % 4 * 4, eps, w[0], w[1], owed);
+        P::store_vectors(lds, turn, i / 64 % ND * 64 + i / 4 % 4 * 16 + i / 16 % 4 * 4 + i % 4, head_of(i), eps, w[0], w[1], owed);
     }
     __syncthreads();
-    const uint8_t *column = lds + (lane % 16) * kStride + 16 * g;
-    constexpr uint32_t kMatrix = Vectors<GT>::planes * kStride;
+    const uint8_t *column = P::column(lds, lane);
     const uint32_t chunks = (c.dim + 63) / 64;
     for (uint32_t t0 = first + 16 * wave; t0 < end; t0 += threads / 4) {
         if (t0 >= length) {
@@ -322,18 +350,16 @@ attention_scores_kernel(AttentionArgs a)
                     delta[2 * j + 1] = v.b;
                 }
             };
-            auto words = [&](int p, MatrixDigits &d) {
-                draw_digits(d, [&](int j) { return z0 + (uint64_t)(2 * (8 * (j / 2) + j % 2) + p) * kGamma; });
-            };
-            multiply_three<GT, (GT <= 4)>(sums, at, kMatrix, kStride, numbers, words);
+            auto state = [&](int p, int j) { return z0 + (uint64_t)(2 * (8 * (j / 2) + j % 2) + p) * kGamma; };
+            P::multiply_three(sums, at, numbers, state);
             z0 += 128 * kGamma;
-            at += 64;
+            at += P::per_64;
         }
         uint64_t mine[4], other[4];
         join_digits<GT>(sums, lane, owed, mine);
 #pragma unroll
         for (int r = 0; r < 4; ++r) other[r] = __shfl_xor((unsigned long long)mine[r], GT, 64);
-uint32_t l = lane;
+        uint32_t l = lane;
         settle(l);                                            // (nothing of this stays in registers from tile to tile)
         const uint32_t head = l % GT;
         const RowShare<GT> own(l);
@@ -356,14 +382,14 @@ uint32_t l = lane;
 }
 
 // The product with the values.  A wavefront has 16 dimensions, the rows of its tile, and lane l takes 16 of every 64 positions; the workgroup, up to 128 dimensions,
-// makes the weights' vectors of 128 positions at a time.
+// makes the weights' vectors of CHUNK positions at a time.
 template <int GT, int CHUNK>
 __global__ void __launch_bounds__(kAttentionBlock, 4)
 attention_values_kernel(AttentionArgs a)
 {
     const uint32_t threads = blockDim.x;                      // 64 for every 16 dimensions
-    constexpr uint32_t kStride = CHUNK + 16;
-    __shared__ __align__(16) uint8_t lds[3 * Vectors<GT>::planes * kStride];
+    using P = Planes<GT, (GT <= 4), CHUNK>;
+    __shared__ __align__(16) uint8_t lds[P::bytes];
     __shared__ unsigned long long owed[2 * GT];
     __shared__ uint64_t row_at[CHUNK], row_state[CHUNK];      // a position's numbers and masks
     const CacheView &c = a.cache;
@@ -374,9 +400,8 @@ attention_values_kernel(AttentionArgs a)
     const uint32_t lane = threadIdx.x % 64, g = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint32_t dim0 = blockIdx.z * (kAttentionWaves * 16) + 16 * wave, dim = dim0 + lane % 16 < c.dim ? dim0 + lane % 16 : 0;
     if (first >= length && (length != 0 || a.splits != 1)) return;         // the join does not read it
-    const uint8_t *column = lds + (lane % 16) * kStride + 16 * g;
-    constexpr uint32_t kMatrix = Vectors<GT>::planes * kStride;
-    clear_planes<GT>(lds, kStride, owed, threads);
+    const uint8_t *column = P::column(lds, lane);
+    P::clear(lds, owed, threads);
     __syncthreads();
     const uint64_t z = (uint64_t)(2 * dim) * kGamma;
     const QuadTurn turn(lane);
@@ -393,7 +418,7 @@ attention_values_kernel(AttentionArgs a)
             const bool there = page_of(a, h.b, t, end) >= 0 && asked;
             const uint64_t s = state_of(a.seed_p, 2 * n), a0 = there ? mix64(s) : 0, a1 = there ? mix64(s + kGamma) : 0;
             const uint64_t eps = there ? (p0 - a0) + (p1 - a1) : 0;                        // opened
-            store_vectors<GT>(lds, kStride, turn, i % 4, head, i % CHUNK / 4 * 4, eps, a0, a1, owed);
+            P::store_vectors(lds, turn, i % CHUNK, head, eps, a0, a1, owed);
         }
         for (uint32_t i = thread; i < CHUNK; i += threads) {
             const int64_t page = page_of(a, h.b, t0 + i, end);
@@ -403,14 +428,12 @@ attention_values_kernel(AttentionArgs a)
         }
         __syncthreads();
         for (uint32_t block = 0; block < CHUNK / 64 && t0 + 64 * block < end && c.pages != 0; ++block) {
-auto numbers = [&](uint64_t (&delta)[16]) {
+            auto numbers = [&](uint64_t (&delta)[16]) {
 #pragma unroll
                 for (int j = 0; j < 16; ++j) delta[j] = load_stream(c.values + row_at[64 * block + 16 * g + j] + dim);
             };
-            auto words = [&](int p, MatrixDigits &d) {
-                draw_digits(d, [&](int j) { return row_state[64 * block + 16 * g + j] + (z + (uint64_t)p * kGamma); });
-            };
-            multiply_three<GT, (GT <= 2)>(sums, column + 64 * block, kMatrix, kStride, numbers, words);
+            auto state = [&](int p, int j) { return row_state[64 * block + 16 * g + j] + (z + (uint64_t)p * kGamma); };
+            P::multiply_three(sums, column + P::per_64 * block, numbers, state);
         }
         __syncthreads();
     }
@@ -423,7 +446,7 @@ auto numbers = [&](uint64_t (&delta)[16]) {
     uint64_t y[4];
     join_digits<GT>(sums, lane, owed, y);
     if (a.splits != 1) {
-        if (l % 16 >= Vectors<GT>::nv || head >= h.count) return;
+        if (l % 16 >= (2 * GT) || head >= h.count) return;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const uint32_t to = dim0 + 4 * (l / 16) + r;
