@@ -77,7 +77,9 @@ AttentionLayout attention_layout(const hb_cache *cache, size_t batch, int q_head
     AttentionLayout lay = {};
     const size_t scores = round_up(8 * batch * q_heads * max_len), numbers = batch * q_heads * cache->dim;
     // Positions of a workgroup: what gives every compute unit two workgroups at a time, four where lengths may differ (eight sequences of none to
-    // 4096 145 us, with two 155; 32768 positions of one 183, with four 194, with one 205); no fewer than make the vectors of a workgroup's heads,
+    // 4096, 32 query heads on 8, 145 us, with two 157, with eight 134, but 202 for 190 where all are 4096; 64 of none to 1000 104, 116, 100; seven of none to
+    // 4096 109, 151, 117; 32768 positions of one 183, with four 194, with one 205);
+    // no fewer than make the vectors of a workgroup's heads,
     // which are the same for 16 positions and for 1000, worth their time (eight heads, 2048 positions of four sequences 48 us with 128 at least, 73 with
     // 32; 1000 of one 33 with 64, 40 with 128, 63 with 256).
     const size_t some = batch != 0 ? batch : 1, groups = some * cache->heads * head_chunks(cache, q_heads), pieces = ((batch > 1 ? 1024 : 512) + groups - 1) / groups;
