@@ -110,10 +110,14 @@ void with_heads(int together, const Body &body)
     }
 }
 
+// Wavefronts of a workgroup with so many tiles: four at least, which make the vectors faster (scores of 16 positions of one head of 80, four and
+// zeros written 16 bytes at a time: 11.4 -> 8.0 us).
+unsigned waves(unsigned tiles) { return tiles > hb::kAttentionWaves ? hb::kAttentionWaves : tiles < 4 ? 4 : tiles; }
+
+// Grids: pieces of the length, heads of the cache (with their chunks of query heads), sequences.
 void launch_scores(const hb::AttentionArgs &a, int together, dim3 grid, hipStream_t stream)
 {
-    const unsigned tiles = (a.per_scores + 15) / 16, most = hb::kAttentionWaves;
-    const dim3 block(64 * (tiles < most ? tiles : most));
+    const dim3 block(64 * waves((a.per_scores + 15) / 16));
     with_heads(together, [&](auto heads) {
         constexpr int GT = decltype(heads)::value;
         switch ((a.cache.dim + 63) / 64) {
@@ -127,9 +131,9 @@ void launch_scores(const hb::AttentionArgs &a, int together, dim3 grid, hipStrea
 
 void launch_values(const hb::AttentionArgs &a, int together, dim3 grid, hipStream_t stream)
 {
-    const unsigned tiles = (a.cache.dim + 15) / 16, most = hb::kAttentionWaves;
-    grid.z = (tiles + most - 1) / most;
-    const dim3 block(64 * (grid.z > 1 ? most : tiles));
+    const unsigned tiles = (a.cache.dim + 15) / 16;
+    grid.y *= (tiles + hb::kAttentionWaves - 1) / hb::kAttentionWaves;
+    const dim3 block(64 * waves(tiles));
     with_heads(together, [&](auto heads) {
         constexpr int GT = decltype(heads)::value;
         if (GT >= 4 || a.per_split <= 64) hipLaunchKernelGGL((hb::attention_values_kernel<GT, 64>), grid, block, 0, stream, a);
@@ -259,17 +263,15 @@ int hb_attention(const hb_cache *cache, const int64_t *q0, const int64_t *q1, si
         hipError_t e = hipSuccess;
         if (max_len != 0) {
             const int together = heads_together(cache, q_heads);
-            const uint64_t groups = batch * cache->heads * head_chunks(cache, q_heads);
-            const uint64_t pieces = (max_len + lay.per_scores - 1) / lay.per_scores;
-            if (groups > 0x7fffffffull || pieces > 65535) return HB_EINVAL;
-            launch_scores(a, together, dim3((unsigned)groups, (unsigned)pieces), (hipStream_t)stream);
+            const unsigned heads = (unsigned)(cache->heads * head_chunks(cache, q_heads));          // 2^14 at most
+            launch_scores(a, together, dim3((unsigned)((max_len + lay.per_scores - 1) / lay.per_scores), heads, (unsigned)batch), (hipStream_t)stream);
             e = hipGetLastError();
             if (e == hipSuccess) {
                 e = relu(a.scores[0], a.scores[1], scores, k, hb::stream_word(seed_relu, 0), hb::stream_word(seed_relu, 1), a.scores[0], a.scores[1],
                          (hipStream_t)stream);
             }
             if (e == hipSuccess) {
-                launch_values(a, together, dim3((unsigned)groups, lay.splits), (hipStream_t)stream);
+                launch_values(a, together, dim3(lay.splits, heads, (unsigned)batch), (hipStream_t)stream);
                 e = hipGetLastError();
             }
         }

@@ -53,12 +53,20 @@ static_assert(3ll * 8 * 128 * 128 * kMostPlaces < 1ll << 31, "sums of digit prod
 
 template <int GT, bool WHOLE, int PLACES>
 struct Planes {
-    static constexpr int nv = 2 * GT, zeros = WHOLE ? (GT == 1 ? 8 : 0) : 16, rows = zeros + 8 * nv;          // of one matrix
+    static constexpr int nv = 2 * GT, zeros = WHOLE ? GT == 1 : 16, rows = zeros + 8 * nv;          // of one matrix
     static constexpr uint32_t stride = (WHOLE ? 4 : 1) * PLACES + 16;         // (16 more: rows of 16 fall into different banks)
     static constexpr uint32_t matrix = rows * stride, bytes = 3 * matrix;
     // A lane's part of the columns: of every 64 places lane quarter g has 16 g .. 16 g + 15.
     static constexpr uint32_t per_64 = WHOLE ? 256 : 64;
-    static __device__ __forceinline__ const uint8_t *column(const uint8_t *lds, uint32_t lane) { return lds + lane % 16 * stride + lane / 16 * (per_64 / 4); }
+    struct Column {
+        const uint8_t *at, *high;             // high: for GT = 1, the column of four weights less, or zeros
+        __device__ __forceinline__ Column operator+(uint32_t bytes) const { return Column{at + bytes, high + bytes}; }
+    };
+    static __device__ __forceinline__ Column column(const uint8_t *lds, uint32_t lane)
+    {
+        const uint32_t c = lane % 16, part = lane / 16 * (per_64 / 4);
+        return Column{lds + c * stride + part, lds + (c < 8 ? 0 : c - 7) * stride + part};
+    }
 
     // Place i of vector v.  Four lanes side by side have places 4 n .. 4 n + 3.
     static __device__ __forceinline__ void store(uint8_t *planes, const QuadTurn &turn, uint32_t i, uint32_t v, uint64_t x)
@@ -97,14 +105,14 @@ struct Planes {
     static __device__ __forceinline__ void clear(uint8_t *lds, unsigned long long *owed, uint32_t threads)
     {
         if (threadIdx.x < nv) owed[threadIdx.x] = 0;
-        constexpr uint32_t words = stride / 4;
+        constexpr uint32_t row = stride / 16, before = zeros * row;
+        const i32x4_t none{};
         if constexpr (zeros != 0) {
-            for (uint32_t i = threadIdx.x; i < 3 * zeros * words; i += threads)
-                *reinterpret_cast<uint32_t *>(lds + i / (zeros * words) * matrix + i % (zeros * words) * 4) = 0;
+            for (uint32_t i = threadIdx.x; i < 3 * before; i += threads) *reinterpret_cast<i32x4_t *>(lds + i / before * matrix + i % before * 16) = none;
         }
-        for (uint32_t i = threadIdx.x; i < 8 * GT * words; i += threads) {
-            const uint32_t plane = i / words;
-            *reinterpret_cast<uint32_t *>(lds + matrix + (zeros + plane / GT * nv + plane % GT) * stride + i % words * 4) = 0;
+        for (uint32_t i = threadIdx.x; i < 8 * GT * row; i += threads) {
+            const uint32_t plane = i / row;
+            *reinterpret_cast<i32x4_t *>(lds + matrix + (zeros + plane / GT * nv + plane % GT) * stride + i % row * 16) = none;
         }
     }
 
@@ -112,25 +120,25 @@ struct Planes {
 
     static __device__ __forceinline__ i32x4_t operand(const uint8_t *at) { return *reinterpret_cast<const i32x4_t *>(at); }
     // sums += numbers 4 s .. 4 s + 3 (bytes flipped) of one matrix times its vectors.
-    static __device__ __forceinline__ void multiply(i32x4_t (&sums)[GT], uint64_t z0, uint64_t z1, uint64_t z2, uint64_t z3, int s, const uint8_t *column)
+    static __device__ __forceinline__ void multiply(i32x4_t (&sums)[GT], uint64_t z0, uint64_t z1, uint64_t z2, uint64_t z3, int s, const Column &column)
     {
         const i32x4_t low{(int)z0, (int)z1, (int)z2, (int)z3}, high{(int)(z0 >> 32), (int)(z1 >> 32), (int)(z2 >> 32), (int)(z3 >> 32)};
         i32x4_t right[GT];
 #pragma unroll
         for (int tile = 0; tile < GT; ++tile) {
-            right[tile] = operand(column + (zeros + 16 * tile) * stride + 16 * s);
+            right[tile] = operand(column.at + (zeros + 16 * tile) * stride + 16 * s);
             sums[tile] = mfma_16x16x64(low, right[tile], sums[tile]);
         }
         // the upper halves meet the columns of four weights less
         if constexpr (GT == 1) {
-            sums[0] = mfma_16x16x64(high, operand(column + 16 * s), sums[0]);
+            sums[0] = mfma_16x16x64(high, operand(column.high + 16 * s), sums[0]);
         } else {
 #pragma unroll
             for (int tile = GT / 2; tile < GT; ++tile) sums[tile] = mfma_16x16x64(high, right[tile - GT / 2], sums[tile]);
         }
     }
     // The same of digits of all 16.
-    static __device__ __forceinline__ void multiply(i32x4_t (&sums)[GT], const Digits &d, const uint8_t *column)
+    static __device__ __forceinline__ void multiply(i32x4_t (&sums)[GT], const Digits &d, const Column &column)
     {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -138,7 +146,7 @@ struct Planes {
 #pragma unroll
             for (int tile = 0; tile < GT; ++tile) {
                 if (i * nv > 16 * tile + 15) continue;
-                sums[tile] = mfma_16x16x64(left, operand(column + (zeros + 16 * tile - i * nv) * stride), sums[tile]);
+                sums[tile] = mfma_16x16x64(left, operand(column.at + (zeros + 16 * tile - i * nv) * stride), sums[tile]);
             }
         }
     }
@@ -154,7 +162,7 @@ struct Planes {
     // Words are drawn eight in step (four: 1 to 4 % slower; 16: as fast).  The loads are under way while words are drawn, but for GT = 8, where the
     // 32 registers that they hold would be the fifth wavefront's on a SIMD.
     template <class Numbers, class State>
-    static __device__ __forceinline__ void multiply_three(i32x4_t (&sums)[GT], const uint8_t *column, const Numbers &numbers, const State &state)
+    static __device__ __forceinline__ void multiply_three(i32x4_t (&sums)[GT], const Column &column, const Numbers &numbers, const State &state)
     {
         uint64_t delta[16];
         Digits d;
@@ -256,17 +264,22 @@ __device__ __forceinline__ int64_t page_of(const AttentionArgs &a, uint32_t b, u
 struct HeadChunk {
     uint32_t b, head, first, count;       // query heads first .. first + count - 1
 };
-// Sequences begin one further with every piece of their lengths: workgroups go to the dies and to the parts of a die in turn, and with the same order for every
-// piece the longest sequences' would meet in one of them (four sequences of none to 8192, 8 heads of 64, 87 -> 73 us; sixteen of none to 4096, two heads
-// of 128, 122 -> 104).
 template <int GT>
 __device__ __forceinline__ HeadChunk head_chunk(const AttentionArgs &a, uint32_t index)
 {
     const uint32_t group = a.q_heads / a.cache.heads, chunks = (group + GT - 1) / GT;
-    const uint32_t chunk = index % chunks, head = index / chunks % a.cache.heads;
-    const uint32_t b = (index / chunks / a.cache.heads + blockIdx.y) % a.batch;
-    const uint32_t left = group - chunk * GT;
-    return HeadChunk{b, head, head * group + chunk * GT, left < GT ? left : GT};
+    const uint32_t chunk = index % chunks, head = index / chunks, left = group - chunk * GT;
+    return HeadChunk{blockIdx.z, head, head * group + chunk * GT, left < GT ? left : GT};
+}
+
+// The piece of the length that a workgroup has.  Workgroups go to the dies and to the parts of a die in turn.  Pieces come first in a grid and begin a golden
+// section of their number further with every head and sequence: the pieces behind the ends of sequences, which have nothing to do, and with them the others,
+// are then spread over all parts (heads first, the same order for every piece: four sequences of none to 8192, 8 heads of 64, 87 us for 71, sixteen of none to
+// 4096, two heads of 128, 122 for 105; sequences one further with every piece: three of none to 5000 73 for 63).
+__device__ __forceinline__ uint32_t piece_of()
+{
+    const uint32_t turn = __umulhi((blockIdx.y + gridDim.y * blockIdx.z) * 0x9E3779B9u, gridDim.x), piece = blockIdx.x + turn;
+    return piece < gridDim.x ? piece : piece - gridDim.x;
 }
 
 // Scores.  A wavefront takes 16 positions at a time: a row of its tile is a key, lane l has row l mod 16 and of every 64 dimensions the pairs
@@ -279,8 +292,8 @@ attention_scores_kernel(AttentionArgs a)
     __shared__ __align__(16) uint8_t lds[P::bytes];
     __shared__ unsigned long long owed[2 * GT];
     const CacheView &c = a.cache;
-    const HeadChunk h = head_chunk<GT>(a, blockIdx.x);
-    const uint32_t threads = blockDim.x;                      // 64 for every 16 positions, up to kAttentionBlock
+    const HeadChunk h = head_chunk<GT>(a, blockIdx.y);
+    const uint32_t threads = blockDim.x;                      // 64 for every 16 positions, from 256 to kAttentionBlock
     const uint32_t lane = threadIdx.x % 64, g = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint64_t row0 = (uint64_t)h.b * a.q_heads + h.first;
     // The queries' numbers, one a thread, in the order of their bytes in the planes: four consecutive ones are two pairs of dimensions.  A thread's first
@@ -296,7 +309,7 @@ attention_scores_kernel(AttentionArgs a)
         q1 = a.q[1][at];
     };
     load_number(threadIdx.x < kNumbers ? threadIdx.x : 0);
-    const uint32_t first = blockIdx.y * a.per_scores, length = __builtin_amdgcn_readfirstlane(c.pages != 0 ? length_of(a, h.b) : 0);
+    const uint32_t first = piece_of() * a.per_scores, length = __builtin_amdgcn_readfirstlane(c.pages != 0 ? length_of(a, h.b) : 0);
     const uint32_t end = first + a.per_scores < a.max_len ? first + a.per_scores : a.max_len;
     auto store_zeros = [&](uint32_t from, uint32_t to, uint32_t thread, uint32_t of) {     // behind the sequence's end
         for (uint32_t i = thread; i < h.count * (to - from); i += of) {
@@ -331,7 +344,7 @@ attention_scores_kernel(AttentionArgs a)
         P::store_vectors(lds, turn, i / 64 % ND * 64 + i / 4 % 4 * 16 + i / 16 % 4 * 4 + i % 4, head_of(i), eps, w[0], w[1], owed);
     }
     __syncthreads();
-    const uint8_t *column = P::column(lds, lane);
+    const typename P::Column column = P::column(lds, lane);
     const uint32_t chunks = (c.dim + 63) / 64;
     for (uint32_t t0 = first + 16 * wave; t0 < end; t0 += threads / 4) {
         if (t0 >= length) {
@@ -341,7 +354,7 @@ attention_scores_kernel(AttentionArgs a)
         if (t0 != first + 16 * wave) look_up(t0);
         uint64_t z0 = state_of(stream_word(seed, 0), 2 * (place + 2 * g));
         i32x4_t sums[GT] = {};
-        const uint8_t *at = column;
+        typename P::Column at = column;
 #pragma unroll 1
         for (uint32_t chunk = 0; chunk < chunks; ++chunk) {
             auto numbers = [&](uint64_t (&delta)[16]) {
@@ -357,7 +370,7 @@ attention_scores_kernel(AttentionArgs a)
             auto state = [&](int p, int j) { return z0 + (uint64_t)(2 * (8 * (j / 2) + j % 2) + p) * kGamma; };
             P::multiply_three(sums, at, numbers, state);
             z0 += 128 * kGamma;
-            at += P::per_64;
+            at = at + P::per_64;
         }
         uint64_t mine[4], other[4];
         join_digits<GT>(sums, lane, owed, mine);
@@ -391,20 +404,21 @@ template <int GT, int CHUNK>
 __global__ void __launch_bounds__(kAttentionBlock, 4)
 attention_values_kernel(AttentionArgs a)
 {
-    const uint32_t threads = blockDim.x;                      // 64 for every 16 dimensions
+    const uint32_t threads = blockDim.x;                      // 64 for every 16 dimensions, 256 at least
     using P = Planes<GT, (GT <= 4), CHUNK>;
     __shared__ __align__(16) uint8_t lds[P::bytes];
     __shared__ unsigned long long owed[2 * GT];
     __shared__ uint64_t row_at[CHUNK], row_state[CHUNK];      // a position's numbers and masks
     const CacheView &c = a.cache;
-    const HeadChunk h = head_chunk<GT>(a, blockIdx.x);
+    const uint32_t halves = (c.dim + kAttentionWaves * 16 - 1) / (kAttentionWaves * 16);       // a workgroup each
+    const HeadChunk h = head_chunk<GT>(a, blockIdx.y / halves);
     const uint32_t length = __builtin_amdgcn_readfirstlane(length_of(a, h.b));
-    const uint32_t first = blockIdx.y * a.per_split, end = first + a.per_split < length ? first + a.per_split : length;
+    const uint32_t split = piece_of(), first = split * a.per_split, end = first + a.per_split < length ? first + a.per_split : length;
     const uint64_t row0 = (uint64_t)h.b * a.q_heads + h.first;
     const uint32_t lane = threadIdx.x % 64, g = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const uint32_t dim0 = blockIdx.z * (kAttentionWaves * 16) + 16 * wave, dim = dim0 + lane % 16 < c.dim ? dim0 + lane % 16 : 0;
+    const uint32_t dim0 = blockIdx.y % halves * (kAttentionWaves * 16) + 16 * wave, dim = dim0 + lane % 16 < c.dim ? dim0 + lane % 16 : 0;
     if (first >= length && (length != 0 || a.splits != 1)) return;         // the join does not read it
-    const uint8_t *column = P::column(lds, lane);
+    const typename P::Column column = P::column(lds, lane);
     P::clear(lds, owed, threads);
     __syncthreads();
     const uint64_t z = (uint64_t)(2 * dim) * kGamma;
@@ -431,7 +445,7 @@ attention_values_kernel(AttentionArgs a)
             row_state[i] = page >= 0 ? state_of(stream_word(c.page_seeds[page], 1), 2 * place) : 0;
         }
         __syncthreads();
-        for (uint32_t block = 0; block < CHUNK / 64 && t0 + 64 * block < end && c.pages != 0; ++block) {
+        for (uint32_t block = 0; block < CHUNK / 64 && t0 + 64 * block < end && c.pages != 0 && dim0 < c.dim; ++block) {
             auto numbers = [&](uint64_t (&delta)[16]) {
 #pragma unroll
                 for (int j = 0; j < 16; ++j) delta[j] = load_stream(c.values + row_at[64 * block + 16 * g + j] + dim);
@@ -454,7 +468,7 @@ attention_values_kernel(AttentionArgs a)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const uint32_t to = dim0 + 4 * (l / 16) + r;
-            if (to < c.dim) a.parts[(2 * (uint64_t)blockIdx.y + party1) * numbers + (row0 + head) * c.dim + to] = y[r];
+            if (to < c.dim) a.parts[(2 * (uint64_t)split + party1) * numbers + (row0 + head) * c.dim + to] = y[r];
         }
         return;
     }
