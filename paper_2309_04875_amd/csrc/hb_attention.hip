@@ -3,6 +3,7 @@
 #include "hb_check.hpp"
 #include "hb_launch.hpp"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace {
@@ -48,10 +49,12 @@ bool append_shape(size_t tokens, uint64_t groups, hb::AppendShape &shape)
 
 size_t round_up(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Workspace of hb_attention: shares of the scores, then the splits' partial sums.
+// Workspace of hb_attention: shares of the scores, then the pieces' partial sums.
 struct AttentionLayout {
     size_t scores1, parts, bytes;
-    uint32_t splits, per_split, per_scores;
+    size_t score_pieces, value_pieces;                        // grids: pieces of a head, of all sequences (together != 0) or of the longest
+    uint32_t least_scores, least_values, together, waves;     // as in AttentionArgs; wavefronts of a workgroup of the scores
+    bool single;
 };
 
 bool attention_sizes(const hb_cache *cache, size_t batch, int q_heads, size_t max_len)
@@ -72,29 +75,45 @@ size_t head_chunks(const hb_cache *cache, int q_heads)
     return (size_t)((group + together - 1) / together);
 }
 
+// Wavefronts of a workgroup with so many tiles: four at least, which make the vectors faster (scores of 16 positions of one head of 80, four and
+// zeros written 16 bytes at a time: 11.4 -> 8.0 us).
+unsigned waves(size_t tiles) { return tiles > (size_t) hb::kAttentionWaves ? hb::kAttentionWaves : tiles < 4 ? 4 : (unsigned)tiles; }
+
 AttentionLayout attention_layout(const hb_cache *cache, size_t batch, int q_heads, size_t max_len)
 {
     AttentionLayout lay = {};
-    const size_t scores = round_up(8 * batch * q_heads * max_len), numbers = batch * q_heads * cache->dim;
-    // Positions of a workgroup: what gives every compute unit two workgroups at a time, four where lengths may differ (eight sequences of none to
-    // 4096, 32 query heads on 8, 145 us, with two 157, with eight 134, but 202 for 190 where all are 4096; 64 of none to 1000 104, 116, 100; seven of none to
-    // 4096 109, 151, 117; 32768 positions of one 183, with four 194, with one 205);
-    // no fewer than make the vectors of a workgroup's heads,
-    // which are the same for 16 positions and for 1000, worth their time (eight heads, 2048 positions of four sequences 48 us with 128 at least, 73 with
-    // 32; 1000 of one 33 with 64, 40 with 128, 63 with 256).
-    const size_t some = batch != 0 ? batch : 1, groups = some * cache->heads * head_chunks(cache, q_heads), pieces = ((batch > 1 ? 1024 : 512) + groups - 1) / groups;
-    const int together = heads_together(cache, q_heads);
-    const size_t least = together < 8 ? 16 * together : groups * ((max_len + 63) / 64) <= 256 ? 64 : 128;
-    size_t per = (max_len + pieces - 1) / pieces;
-    if (per < least) per = least;
-    per = per > 64 ? (per + 127) / 128 * 128 : per > 32 ? 64 : per > 16 ? 32 : 16;
-    if (per > hb::kMostPlaces) per = hb::kMostPlaces;
-    lay.per_scores = (uint32_t)per;
-    lay.per_split = (uint32_t)(per < 64 ? 64 : per);
-    lay.splits = (uint32_t)((max_len + lay.per_split - 1) / lay.per_split);
+    const size_t scores = round_up(8 * batch * q_heads * max_len), numbers = q_heads * cache->dim;
+    // Workgroups: two at a time for every compute unit, 512, if that gives every sequence two pieces or more (32768 positions of one sequence 183 us, with
+    // 1024 194, with 256 205).  Otherwise pieces of one size, 1024 workgroups or more (64 sequences of none to 1000, four heads, cut so: 104 us, with
+    // 512 116, with 2048 100, but eight of 4096 each 202 then, 190 with 1024).
+    // No fewer positions than make the vectors of a workgroup's heads, which are the same for 16 positions and for 1000, worth their time (eight heads, 2048
+    // positions of four sequences 48 us with 128 at least, 73 with 32; 1000 of one 33 with 64, 40 with 128, 63 with 256).
+    const size_t some = batch != 0 ? batch : 1, heads = cache->heads * head_chunks(cache, q_heads), groups = some * heads;
+    const int query_heads = heads_together(cache, q_heads);
+    const size_t worth = query_heads < 8 ? 16 * query_heads : groups * ((max_len + 63) / 64) <= 256 ? 64 : 128;
+    auto units = [](size_t n, size_t unit) { return (n + unit - 1) / unit; };
+    auto size = [&](size_t workgroups) {                      // of a piece, where all sequences are of the greatest length
+        const size_t each = units(max_len, units(workgroups, groups));
+        return each < worth ? worth : each > hb::kMostPlaces ? hb::kMostPlaces : each;
+    };
+    const bool together = batch <= 64 && 512 / heads >= 2 * some && max_len > hb::kValueUnit * units(worth, hb::kValueUnit);
+    const size_t least = together ? worth : size(1024);
+    lay.least_scores = (uint32_t)units(least, hb::kScoreUnit);
+    lay.least_values = (uint32_t)units(least, hb::kValueUnit);
+    lay.together = together ? (uint32_t)(512 / heads) : 0;
+    lay.waves = waves(units(size(512), 16));
+    lay.score_pieces = units(max_len, hb::kScoreUnit * lay.least_scores);
+    lay.value_pieces = units(max_len, hb::kValueUnit * lay.least_values);
+    lay.single = lay.value_pieces <= 1;
+    if (together) {
+        // as many as are meant to be, or as one sum's most places make
+        const size_t most = batch * units(max_len, hb::kMostPlaces);
+        lay.score_pieces = std::min<size_t>(lay.together, batch * lay.score_pieces);
+        lay.value_pieces = std::min(std::max<size_t>(lay.together, most), batch * lay.value_pieces);
+    }
     lay.scores1 = scores;
     lay.parts = 2 * scores;
-    lay.bytes = 2 * scores + round_up(16 * numbers * lay.splits);
+    lay.bytes = 2 * scores + (lay.single ? 0 : round_up(16 * numbers * lay.value_pieces * (together ? 1 : batch)));
     return lay;
 }
 
@@ -110,14 +129,16 @@ void with_heads(int together, const Body &body)
     }
 }
 
-// Wavefronts of a workgroup with so many tiles: four at least, which make the vectors faster (scores of 16 positions of one head of 80, four and
-// zeros written 16 bytes at a time: 11.4 -> 8.0 us).
-unsigned waves(unsigned tiles) { return tiles > hb::kAttentionWaves ? hb::kAttentionWaves : tiles < 4 ? 4 : tiles; }
-
-// Grids: pieces of the length, heads of the cache (with their chunks of query heads), sequences.
-void launch_scores(const hb::AttentionArgs &a, int together, dim3 grid, hipStream_t stream)
+// Grids: heads of the cache (with their chunks of query heads); pieces, or sequences and pieces of each.
+dim3 grid_of(size_t heads, const AttentionLayout &lay, size_t batch, size_t pieces)
 {
-    const dim3 block(64 * waves((a.per_scores + 15) / 16));
+    if (lay.together == 0) return dim3((unsigned)heads, (unsigned)batch, (unsigned)pieces);
+    const size_t y = std::min<size_t>(pieces, 32768);
+    return dim3((unsigned)heads, (unsigned)y, (unsigned)((pieces + y - 1) / y));
+}
+
+void launch_scores(const hb::AttentionArgs &a, int together, dim3 grid, dim3 block, hipStream_t stream)
+{
     with_heads(together, [&](auto heads) {
         constexpr int GT = decltype(heads)::value;
         switch ((a.cache.dim + 63) / 64) {
@@ -132,11 +153,11 @@ void launch_scores(const hb::AttentionArgs &a, int together, dim3 grid, hipStrea
 void launch_values(const hb::AttentionArgs &a, int together, dim3 grid, hipStream_t stream)
 {
     const unsigned tiles = (a.cache.dim + 15) / 16;
-    grid.y *= (tiles + hb::kAttentionWaves - 1) / hb::kAttentionWaves;
+    grid.x *= (tiles + hb::kAttentionWaves - 1) / hb::kAttentionWaves;
     const dim3 block(64 * waves(tiles));
     with_heads(together, [&](auto heads) {
         constexpr int GT = decltype(heads)::value;
-        if (GT >= 4 || a.per_split <= 64) hipLaunchKernelGGL((hb::attention_values_kernel<GT, 64>), grid, block, 0, stream, a);
+        if (GT >= 4 || a.least_values == 1) hipLaunchKernelGGL((hb::attention_values_kernel<GT, 64>), grid, block, 0, stream, a);
         else hipLaunchKernelGGL((hb::attention_values_kernel<GT, GT >= 4 ? 64 : 128>), grid, block, 0, stream, a);
     });
 }
@@ -255,27 +276,28 @@ int hb_attention(const hb_cache *cache, const int64_t *q0, const int64_t *q1, si
         a.batch = (uint32_t)batch;
         a.q_heads = (uint32_t)q_heads;
         a.max_len = (uint32_t)max_len;
-        a.splits = lay.splits;
-        a.per_scores = lay.per_scores;
-        a.per_split = lay.per_split;
+        a.least_scores = lay.least_scores;
+        a.least_values = lay.least_values;
+        a.together = lay.together;
+        a.single = lay.single;
         const hb::GroupLauncher relu = hb::launcher_table().f[hb::kRelu][m - k - 1];
         if (relu == nullptr) return hb::fail_hip(hipErrorInvalidDeviceFunction, "no kernel was built for this slice width");
         hipError_t e = hipSuccess;
         if (max_len != 0) {
             const int together = heads_together(cache, q_heads);
-            const unsigned heads = (unsigned)(cache->heads * head_chunks(cache, q_heads));          // 2^14 at most
-            launch_scores(a, together, dim3((unsigned)((max_len + lay.per_scores - 1) / lay.per_scores), heads, (unsigned)batch), (hipStream_t)stream);
+            const size_t heads = cache->heads * head_chunks(cache, q_heads);                 // 2^14 at most
+            launch_scores(a, together, grid_of(heads, lay, batch, lay.score_pieces), dim3(64 * lay.waves), (hipStream_t)stream);
             e = hipGetLastError();
             if (e == hipSuccess) {
                 e = relu(a.scores[0], a.scores[1], scores, k, hb::stream_word(seed_relu, 0), hb::stream_word(seed_relu, 1), a.scores[0], a.scores[1],
                          (hipStream_t)stream);
             }
             if (e == hipSuccess) {
-                launch_values(a, together, dim3(lay.splits, heads, (unsigned)batch), (hipStream_t)stream);
+                launch_values(a, together, grid_of(heads, lay, batch, lay.value_pieces), (hipStream_t)stream);
                 e = hipGetLastError();
             }
         }
-        if (e == hipSuccess && lay.splits != 1) {
+        if (e == hipSuccess && !(lay.single && max_len != 0)) {
             const unsigned over = (unsigned)(((uint64_t)q_heads * cache->dim + hb::kJoinNumbers - 1) / hb::kJoinNumbers);
             hipLaunchKernelGGL(hb::attention_join_kernel, dim3(over, (unsigned)batch), dim3(hb::kJoinBlock), 0, (hipStream_t)stream, a);
             e = hipGetLastError();

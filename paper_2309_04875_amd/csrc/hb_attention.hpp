@@ -12,17 +12,87 @@ struct AttentionArgs {
     const uint64_t *q[2];                 // [batch][q_heads][dim]
     uint64_t *out[2];
     uint64_t *scores[2];                  // [batch][q_heads][max_len], workspace
-    uint64_t *parts;                      // [splits][2][batch][q_heads][dim], workspace
+    uint64_t *parts;                      // [pieces of the values][2][q_heads][dim], workspace
     const int32_t *table, *lens;          // [batch][table_width], [batch]
     uint64_t table_width;
     uint64_t seed_q, seed_s, seed_p, seed_o;
-    uint32_t batch, q_heads, max_len, splits, per_scores, per_split;    // per_..: positions of a workgroup
+    uint32_t batch, q_heads, max_len;
+    // A piece is the positions that a workgroup has: `least` units or more.  together: how many pieces all sequences are cut into; 0: every sequence by itself
+    // into pieces of the least size.  single: no sequence has more than one piece of the values.
+    uint32_t least_scores, least_values, together, single;
 };
 
 __device__ __forceinline__ uint32_t length_of(const AttentionArgs &a, uint32_t b)
 {
     const int32_t n = a.lens[b];
     return n < 0 ? 0 : ((uint32_t)n > a.max_len ? a.max_len : (uint32_t)n);
+}
+
+// How the sequences are cut.  Their lengths are the device's alone, and max_len may be far above them: each workgroup works out for itself, a sequence a lane (64
+// at most), the smallest size of a piece that makes no more than a.together pieces, and which piece is its own.  That number is what the card holds at a
+// time: eight sequences of none to 4096 of 128, 32 query heads on 8, 117 us; 145 cut after max_len, where 67 pieces a head came and 64 fit (16 of two
+// heads of 128 94 and 105; 128 positions of one 19.7 and 19.1: the cutting itself).  Where sequences and heads are too many, pieces are of one size, and
+// begin with another sequence for every piece of the length: with the same order the longest would meet in a part of the card, since workgroups go to the
+// dies and their parts in turn (sixteen sequences, two heads, 122 us, 104 so).
+constexpr uint32_t kScoreUnit = 16, kValueUnit = 64;
+constexpr uint32_t kMostPlaces = 1 << 12;                     // positions that one sum takes (below)
+
+struct Cut {
+    uint32_t length, upto, pieces, size;                      // a sequence's length, its pieces, and those up to and with it; positions of a piece
+};
+// Inclusive sums over a row of 16 lanes.
+__device__ __forceinline__ uint32_t row_scan(uint32_t v)
+{
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xF, 0xF, true);       // from one lane below, two, four, eight
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xF, 0xF, true);
+    return v + __builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xF, 0xF, true);
+}
+template <uint32_t UNIT>
+__device__ __forceinline__ Cut cut_sequences(const AttentionArgs &a, uint32_t lane, uint32_t least)
+{
+    const uint32_t length = lane < a.batch ? length_of(a, lane) : 0, units = (length + UNIT - 1) / UNIT;
+    uint32_t pieces = units, scan = row_scan(units), each = least;
+    auto row = [&](int r) { return (uint32_t)__builtin_amdgcn_readlane(scan, 16 * r + 15); };
+    const uint32_t all = row(0) + row(1) + row(2) + row(3);
+    if (all > each * a.together) each = __builtin_amdgcn_readfirstlane((all + a.together - 1) / a.together);
+    for (;; each += each / 16 + 1) {
+        const bool most = UNIT == kValueUnit && each >= kMostPlaces / UNIT;
+        if (most) each = kMostPlaces / UNIT;
+        if (each != 1) {
+            pieces = (units + each - 1) / each;
+            scan = row_scan(pieces);
+        }
+        const uint32_t r0 = row(0), r1 = r0 + row(1), r2 = r1 + row(2);
+        if (r2 + row(3) <= a.together || most) return Cut{length, scan + (lane < 16 ? 0 : lane < 32 ? r0 : lane < 48 ? r1 : r2), pieces, each * UNIT};
+    }
+}
+
+// The piece of this workgroup: positions first to end (none: nothing to do) of sequence b.  part: its number among all.
+struct Piece {
+    uint32_t b, length, first, end, part;
+};
+template <uint32_t UNIT>
+__device__ __forceinline__ Piece piece_of(const AttentionArgs &a, uint32_t lane, uint32_t least)
+{
+    uint32_t b, length, split, size, part;
+    if (a.together == 0) {
+        b = (blockIdx.y + blockIdx.z) % a.batch;
+        length = __builtin_amdgcn_readfirstlane(length_of(a, b));
+        split = blockIdx.z;
+        size = least * UNIT;
+        part = split * a.batch + b;
+    } else {
+        const Cut cut = cut_sequences<UNIT>(a, lane, least);
+        part = blockIdx.y + blockIdx.z * gridDim.y;
+        b = __builtin_popcountll(__ballot(cut.upto <= part));
+        if (b >= a.batch) return Piece{0, 0, 0, 0, 0};
+        length = __builtin_amdgcn_readlane(cut.length, b);
+        split = part - (__builtin_amdgcn_readlane(cut.upto, b) - __builtin_amdgcn_readlane(cut.pieces, b));
+        size = __builtin_amdgcn_readfirstlane(cut.size);
+    }
+    const uint32_t first = split * size, left = first < length ? length - first : 0;
+    return Piece{b, length, first, first + (left < size ? left : size), part};
 }
 
 constexpr int kAttentionBlock = 512, kAttentionWaves = kAttentionBlock / 64, kJoinBlock = 256;
@@ -48,7 +118,6 @@ constexpr int kAttentionBlock = 512, kAttentionWaves = kAttentionBlock / 64, kJo
 // write and to hold: it is for one or two heads at a time (32 heads of 4096 positions of 128, one query head each, 85 -> 78 us; 8192 of 8 heads 53 -> 49; eight
 // sequences of none to 4096 with two 126 -> 117) and, 64 positions at a time, for the values of four (2 x 4096 of 192 110 -> 104, 4 x 1000 of 128 40 -> 39; their
 // scores stay as they were, or with few positions lose: 39 -> 46).
-constexpr int kMostPlaces = 1 << 12;
 static_assert(3ll * 8 * 128 * 128 * kMostPlaces < 1ll << 31, "sums of digit products");
 
 template <int GT, bool WHOLE, int PLACES>
@@ -217,8 +286,9 @@ __device__ __forceinline__ void join_digits(const i32x4_t (&sums)[GT], uint32_t 
 #pragma unroll
         for (int tile = 0; tile < GT; ++tile) y += (uint64_t)(int64_t)sums[tile][r] << (8 * kPer * tile);
         if constexpr (kPer > 1) y *= weight;
-#pragma unroll
-        for (int step = (2 * GT); step < 16; step *= 2) y += __shfl_xor((unsigned long long)y, step, 64);
+        if constexpr (GT <= 1) y += across<2>(y);
+        if constexpr (GT <= 2) y += across<4>(y);
+        if constexpr (GT <= 4) y += across<8>(y);
         value[r] = y + owed[lane % (2 * GT)];
     }
 }
@@ -260,26 +330,16 @@ __device__ __forceinline__ int64_t page_of(const AttentionArgs &a, uint32_t b, u
     return page < (int64_t)a.cache.pages ? page : -1;
 }
 
-// What a workgroup works on: a sequence, a head of the cache and up to GT of its query heads.
+// What a workgroup works on beside its piece: a head of the cache and up to GT of its query heads.
 struct HeadChunk {
-    uint32_t b, head, first, count;       // query heads first .. first + count - 1
+    uint32_t head, first, count;          // query heads first .. first + count - 1
 };
 template <int GT>
 __device__ __forceinline__ HeadChunk head_chunk(const AttentionArgs &a, uint32_t index)
 {
     const uint32_t group = a.q_heads / a.cache.heads, chunks = (group + GT - 1) / GT;
     const uint32_t chunk = index % chunks, head = index / chunks, left = group - chunk * GT;
-    return HeadChunk{blockIdx.z, head, head * group + chunk * GT, left < GT ? left : GT};
-}
-
-// The piece of the length that a workgroup has.  Workgroups go to the dies and to the parts of a die in turn.  Pieces come first in a grid and begin a golden
-// section of their number further with every head and sequence: the pieces behind the ends of sequences, which have nothing to do, and with them the others,
-// are then spread over all parts (heads first, the same order for every piece: four sequences of none to 8192, 8 heads of 64, 87 us for 71, sixteen of none to
-// 4096, two heads of 128, 122 for 105; sequences one further with every piece: three of none to 5000 73 for 63).
-__device__ __forceinline__ uint32_t piece_of()
-{
-    const uint32_t turn = __umulhi((blockIdx.y + gridDim.y * blockIdx.z) * 0x9E3779B9u, gridDim.x), piece = blockIdx.x + turn;
-    return piece < gridDim.x ? piece : piece - gridDim.x;
+    return HeadChunk{head, head * group + chunk * GT, left < GT ? left : GT};
 }
 
 // Scores.  A wavefront takes 16 positions at a time: a row of its tile is a key, lane l has row l mod 16 and of every 64 dimensions the pairs
@@ -292,10 +352,13 @@ attention_scores_kernel(AttentionArgs a)
     __shared__ __align__(16) uint8_t lds[P::bytes];
     __shared__ unsigned long long owed[2 * GT];
     const CacheView &c = a.cache;
-    const HeadChunk h = head_chunk<GT>(a, blockIdx.y);
-    const uint32_t threads = blockDim.x;                      // 64 for every 16 positions, from 256 to kAttentionBlock
+    const HeadChunk h = head_chunk<GT>(a, blockIdx.x);
+    const uint32_t threads = blockDim.x;                      // from 256 to kAttentionBlock
     const uint32_t lane = threadIdx.x % 64, g = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const uint64_t row0 = (uint64_t)h.b * a.q_heads + h.first;
+    const Piece piece = piece_of<kScoreUnit>(a, lane, a.least_scores);
+    const uint32_t first = piece.first, end = piece.end;
+    if (first >= end || c.pages == 0) return;                 // (no score of a position without a key is used)
+    const uint64_t row0 = (uint64_t)piece.b * a.q_heads + h.first;
     // The queries' numbers, one a thread, in the order of their bytes in the planes: four consecutive ones are two pairs of dimensions.  A thread's first
     // is under way before anything is waited for.
     constexpr uint32_t kNumbers = GT * ND * 64;
@@ -309,27 +372,17 @@ attention_scores_kernel(AttentionArgs a)
         q1 = a.q[1][at];
     };
     load_number(threadIdx.x < kNumbers ? threadIdx.x : 0);
-    const uint32_t first = piece_of() * a.per_scores, length = __builtin_amdgcn_readfirstlane(c.pages != 0 ? length_of(a, h.b) : 0);
-    const uint32_t end = first + a.per_scores < a.max_len ? first + a.per_scores : a.max_len;
-    auto store_zeros = [&](uint32_t from, uint32_t to, uint32_t thread, uint32_t of) {     // behind the sequence's end
-        for (uint32_t i = thread; i < h.count * (to - from); i += of) {
-            const uint64_t j = (row0 + i / (to - from)) * a.max_len + from + i % (to - from);
-            a.scores[0][j] = 0;
-            a.scores[1][j] = 0;
-        }
-    };
-    if (first >= length) return store_zeros(first, end, threadIdx.x, threads);
     // The keys of 16 positions, a row each.  One without a key reads the first one's: its score is not used.
     uint64_t there = 0, seed = 0, place = 0;
     const uint64_t *keys = nullptr;
     auto look_up = [&](uint32_t t0) {
-        const int64_t page = page_of(a, h.b, t0 + lane % 16, length);
+        const int64_t page = page_of(a, piece.b, t0 + lane % 16, end);
         there = __ballot(page >= 0);
         place = page >= 0 ? place_in_page(c, h.head, (t0 + lane % 16) % c.page, 0) : 0;
         keys = c.keys + (page >= 0 ? page : 0) * page_numbers(c) + place;
         seed = c.page_seeds[page >= 0 ? page : 0];
     };
-    if (first + 16 * wave < length) look_up(first + 16 * wave);
+    if (first + 16 * wave < end) look_up(first + 16 * wave);
     P::clear(lds, owed, threads);
     __syncthreads();
     const QuadTurn turn(lane);
@@ -347,10 +400,6 @@ attention_scores_kernel(AttentionArgs a)
     const typename P::Column column = P::column(lds, lane);
     const uint32_t chunks = (c.dim + 63) / 64;
     for (uint32_t t0 = first + 16 * wave; t0 < end; t0 += threads / 4) {
-        if (t0 >= length) {
-            store_zeros(t0, t0 + 16 < end ? t0 + 16 : end, lane, 64);
-            continue;
-        }
         if (t0 != first + 16 * wave) look_up(t0);
         uint64_t z0 = state_of(stream_word(seed, 0), 2 * (place + 2 * g));
         i32x4_t sums[GT] = {};
@@ -375,7 +424,7 @@ attention_scores_kernel(AttentionArgs a)
         uint64_t mine[4], other[4];
         join_digits<GT>(sums, lane, owed, mine);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) other[r] = __shfl_xor((unsigned long long)mine[r], GT, 64);
+        for (int r = 0; r < 4; ++r) other[r] = across<GT>(mine[r]);
         uint32_t l = lane;
         settle(l);                                            // (nothing of this stays in registers from tile to tile)
         const uint32_t head = l % GT;
@@ -411,13 +460,13 @@ attention_values_kernel(AttentionArgs a)
     __shared__ uint64_t row_at[CHUNK], row_state[CHUNK];      // a position's numbers and masks
     const CacheView &c = a.cache;
     const uint32_t halves = (c.dim + kAttentionWaves * 16 - 1) / (kAttentionWaves * 16);       // a workgroup each
-    const HeadChunk h = head_chunk<GT>(a, blockIdx.y / halves);
-    const uint32_t length = __builtin_amdgcn_readfirstlane(length_of(a, h.b));
-    const uint32_t split = piece_of(), first = split * a.per_split, end = first + a.per_split < length ? first + a.per_split : length;
-    const uint64_t row0 = (uint64_t)h.b * a.q_heads + h.first;
+    const HeadChunk h = head_chunk<GT>(a, blockIdx.x / halves);
     const uint32_t lane = threadIdx.x % 64, g = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const uint32_t dim0 = blockIdx.y % halves * (kAttentionWaves * 16) + 16 * wave, dim = dim0 + lane % 16 < c.dim ? dim0 + lane % 16 : 0;
-    if (first >= length && (length != 0 || a.splits != 1)) return;         // the join does not read it
+    const Piece piece = piece_of<kValueUnit>(a, lane, a.least_values);
+    const uint32_t first = piece.first, end = piece.end;
+    if (first >= end && (piece.length != 0 || !a.single)) return;          // the join does not read it
+    const uint64_t row0 = (uint64_t)piece.b * a.q_heads + h.first;
+    const uint32_t dim0 = blockIdx.x % halves * (kAttentionWaves * 16) + 16 * wave, dim = dim0 + lane % 16 < c.dim ? dim0 + lane % 16 : 0;
     const typename P::Column column = P::column(lds, lane);
     P::clear(lds, owed, threads);
     __syncthreads();
@@ -433,13 +482,13 @@ attention_values_kernel(AttentionArgs a)
             const bool asked = head < h.count && t < end;
             const uint64_t n = (row0 + (asked ? head : 0)) * a.max_len + (asked ? t : first);
             const uint64_t p0 = a.scores[0][n], p1 = a.scores[1][n];
-            const bool there = page_of(a, h.b, t, end) >= 0 && asked;
+            const bool there = page_of(a, piece.b, t, end) >= 0 && asked;
             const uint64_t s = state_of(a.seed_p, 2 * n), a0 = there ? mix64(s) : 0, a1 = there ? mix64(s + kGamma) : 0;
             const uint64_t eps = there ? (p0 - a0) + (p1 - a1) : 0;                        // opened
             P::store_vectors(lds, turn, i % CHUNK, head, eps, a0, a1, owed);
         }
         for (uint32_t i = thread; i < CHUNK; i += threads) {
-            const int64_t page = page_of(a, h.b, t0 + i, end);
+            const int64_t page = page_of(a, piece.b, t0 + i, end);
             const uint64_t place = place_in_page(c, h.head, (t0 + i) % c.page, 0);
             row_at[i] = page >= 0 ? page * page_numbers(c) + place : 0;       // without a value: the first one's, times zeros
             row_state[i] = page >= 0 ? state_of(stream_word(c.page_seeds[page], 1), 2 * place) : 0;
@@ -456,25 +505,24 @@ attention_values_kernel(AttentionArgs a)
         __syncthreads();
     }
     // Of each number and party one partial sum, or the result where there is one split.
-    const uint64_t numbers = (uint64_t)a.batch * a.q_heads * c.dim;
     uint32_t l = lane;
     settle(l);
     const uint32_t head = l % GT;
     const bool party1 = (l & GT) != 0;
     uint64_t y[4];
     join_digits<GT>(sums, lane, owed, y);
-    if (a.splits != 1) {
+    if (!a.single) {
         if (l % 16 >= (2 * GT) || head >= h.count) return;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const uint32_t to = dim0 + 4 * (l / 16) + r;
-            if (to < c.dim) a.parts[(2 * (uint64_t)split + party1) * numbers + (row0 + head) * c.dim + to] = y[r];
+            if (to < c.dim) a.parts[((2 * (uint64_t)piece.part + party1) * a.q_heads + h.first + head) * c.dim + to] = y[r];
         }
         return;
     }
     uint64_t other[4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) other[r] = __shfl_xor((unsigned long long)y[r], GT, 64);
+    for (int r = 0; r < 4; ++r) other[r] = across<GT>(y[r]);
     const RowShare<GT> mine(l);
     if (!mine.any || head >= h.count) return;
 #pragma unroll
@@ -483,14 +531,14 @@ attention_values_kernel(AttentionArgs a)
         const uint32_t to = dim0 + 4 * (l / 16) + mine.row(x);
         if (to >= c.dim) continue;
         const uint64_t i = (row0 + head) * c.dim + to;
-        const Pair o = finish_output(a, i, length, sum);
+        const Pair o = finish_output(a, i, piece.length, sum);
         a.out[0][i] = o.p0;
         a.out[1][i] = o.p1;
     }
 }
 
-// Joins the splits and divides by the length.  32 numbers a workgroup, whose
-// splits eight threads each share out.
+// Joins a sequence's pieces and divides by the length.  32 numbers a workgroup, whose
+// pieces eight threads each share out.
 constexpr int kJoinNumbers = 32, kJoinShares = kJoinBlock / kJoinNumbers;
 
 __global__ void __launch_bounds__(kJoinBlock)
@@ -499,14 +547,27 @@ attention_join_kernel(AttentionArgs a)
     __shared__ uint64_t partial[2][kJoinShares][kJoinNumbers];
     const uint64_t per = (uint64_t)a.q_heads * a.cache.dim;
     const uint32_t b = blockIdx.y, x = threadIdx.x % kJoinNumbers, share = threadIdx.x / kJoinNumbers, at = blockIdx.x * kJoinNumbers + x;
-    const uint64_t i = b * per + at, numbers = a.batch * per;
-    const uint32_t length = __builtin_amdgcn_readfirstlane(length_of(a, b));
-    const uint32_t splits = (length + a.per_split - 1) / a.per_split;
+    const uint64_t i = b * per + at;
+    uint32_t length, pieces, from, step;                      // the sequence's pieces: from, from + step, ..
+    if (a.together == 0) {
+        const uint32_t size = a.least_values * kValueUnit;
+        length = __builtin_amdgcn_readfirstlane(length_of(a, b));
+        pieces = (length + size - 1) / size;
+        from = b;
+        step = a.batch;
+    } else {
+        const Cut cut = cut_sequences<kValueUnit>(a, threadIdx.x % 64, a.least_values);
+        length = __builtin_amdgcn_readlane(cut.length, b);
+        pieces = __builtin_amdgcn_readlane(cut.pieces, b);
+        from = __builtin_amdgcn_readlane(cut.upto, b) - pieces;
+        step = 1;
+    }
     Pair o{0, 0};
     if (at < per) {
-        for (uint32_t s = share; s < splits; s += kJoinShares) {
-            o.p0 += a.parts[2 * (uint64_t)s * numbers + i];
-            o.p1 += a.parts[(2 * (uint64_t)s + 1) * numbers + i];
+        for (uint32_t s = share; s < pieces; s += kJoinShares) {
+            const uint64_t part = 2 * (uint64_t)(from + s * step) * per + at;
+            o.p0 += a.parts[part];
+            o.p1 += a.parts[part + per];
         }
     }
     partial[0][share][x] = o.p0;

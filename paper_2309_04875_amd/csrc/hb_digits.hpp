@@ -116,6 +116,15 @@ __device__ __forceinline__ uint64_t quad_sum(uint64_t v)
     return v + ((uint64_t)h2 << 32 | l2);
 }
 
+// v of the lane whose number differs by X < 32.
+template <int X>
+__device__ __forceinline__ uint64_t across(uint64_t v)
+{
+    const uint32_t low = (uint32_t)__builtin_amdgcn_ds_swizzle((int)(uint32_t)v, X << 10 | 0x1F);
+    const uint32_t high = (uint32_t)__builtin_amdgcn_ds_swizzle((int)(uint32_t)(v >> 32), X << 10 | 0x1F);
+    return (uint64_t)high << 32 | low;
+}
+
 // c + A B of 16 x 64 by 64 x 16 int8.  Lane l holds 16 numbers of row (A) or column (B) l mod 16 in each of its four registers' bytes, those of
 // the same 16 places of the sum in A and B (lanes l with the same l / 16 share them); which places is the caller's choice.  The result's lane l
 // holds rows 4 (l / 16) .. + 3 of column l mod 16.

@@ -85,6 +85,24 @@ def test_larger(batch, heads, group, dim, page, max_len):
     Case(np.random.default_rng(batch), batch, heads, group, dim, page, max_len).check()
 
 
+@pytest.mark.parametrize("heads,group,dim,page,max_len,lens", [
+    (8, 1, 16, 16, 9000, [5000, 1, 0]), (2, 4, 18, 7, 3001, [0, 0, 3001, 0, 17]), (1, 8, 66, 64, 6000, [130]), (2, 2, 130, 12, 2000, [0, 65, 0, 64, 1999]),
+    (1, 1, 4, 9, 700, [i * i % 301 if i % 5 else 0 for i in range(64)]), (1, 3, 4, 9, 300, [i * i % 301 for i in range(65)]),
+    (256, 1, 2, 64, 8500, [8500]), (128, 1, 2, 64, 9000, [9000, 7000]), (300, 1, 2, 16, 300, [299, 1])])
+def test_sequences_of_any_lengths(heads, group, dim, page, max_len, lens):
+    """Lengths far below the greatest, empty sequences between others, as many sequences as are cut together and one more, pieces as long as a sum may be."""
+    case = Case(np.random.default_rng(dim), len(lens), heads, group, dim, page, max_len, lens)
+    args = case.on_gpu()
+    need = hb.hb_attention_workspace_bytes(case.cache, len(lens), heads * group, max_len)
+    room = torch.full((need + 512,), 0xA5, dtype=torch.uint8, device=du.DEV)
+    want = case.want()
+    for _ in range(2):
+        got = hb.hb_attention(*args, workspace=room[256: 256 + need])
+        for g, w in zip(got, want):
+            assert np.array_equal(du.host(g), w)
+    assert bool((room[:256] == 0xA5).all()) and bool((room[256 + need:] == 0xA5).all())
+
+
 @pytest.mark.parametrize("group,dim", [(1, 64), (3, 18), (4, 128), (8, 40)])
 def test_any_number_of_the_ring(group, dim):
     """Keys, values and queries over all 64 bits: every carry between digits."""
