@@ -341,7 +341,7 @@ HB_API int hb_cache_append(const hb_cache *cache, const int64_t *k0, const int64
  * q0, q1, out0, out1: batch x q_heads x dim.  q_heads: a multiple of heads.  table_width * page >= max_len.
  * Dealer material, with S_j = hb_tensor_seed(seed, j), row = b * q_heads + head, i = row * dim + d, j = row * max_len + t: masks of the query
  * words 2i, 2i + 1 of the stream started at S_0; score j words 5j .. 5j + 4 of S_1 (c_0, then the truncation's); the ReLU is hb_relu's on the
- * tensor batch x q_heads x max_len of scores with seed S_2, shares 0 and 0 behind a sequence's end and in holes; masks of p words 2j, 2j + 1
+ * tensor batch x q_heads x max_len of scores with seed S_2 (elements behind a sequence's end and in holes reach no output); masks of p words 2j, 2j + 1
  * of S_3; output i words 9i .. 9i + 8 of S_4 (c_0, first and second truncation).  A product's party shares, with a the fresh mask, b the cache's, eps =
  * x - a opened now and D = y - b: c_0 + sum eps (b_0 + D) + D a_0 and (sum a b - c_0) + sum eps b_1 + D a_1.
  * workspace: DEVICE, 256-byte aligned, hb_attention_workspace_bytes(cache, batch, q_heads, max_len) bytes (0 for invalid sizes; of `cache` the sizes
