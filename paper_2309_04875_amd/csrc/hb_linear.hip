@@ -29,12 +29,15 @@ hipError_t go(hb::LinearArgs &a, hipStream_t stream)
 //   64 x                                   219     122     122    94.9    59.2    48.1   [37.3]
 //   64 x (4096 -> 16384)                   886     494     503     384     240     187    [116]
 //    8 x (512 -> 512)                      3.8    [4.1]    3.9     3.9     4.9     6.3     8.0
+// Eight rows by sixteen tiles, with groups of 128, halve the digits to be made and read for each weight, at two wavefronts a SIMD for four: from two rounds of
+// the last on they are 4 to 11 % faster (64 x (4096 -> 16384) 109 for 113, 128 x (4096 -> 4096) 51 for 58, 512 x (1024 -> 2048) 37 for 41, but
+// 64 x (4096 -> 4096) 50 for 36).  Scaling every 64 or 32 inputs takes the registers of the second tile.
 // One row of many outputs (16384: 13.1 instead of 17.7) shares its digits among four tiles; up to 1024 inputs, four steps, it needs no sixteen
 // wavefronts (512 -> 1000 4.0 instead of 4.5).
 struct Form {
     uint64_t rows, tiles, round;
 };
-constexpr Form kForms[] = {{1, 1, 38}, {2, 1, 41}, {2, 2, 75}, {2, 4, 120}, {4, 4, 143}, {8, 4, 227}, {8, 8, 345}, {1, 4, 105}};
+constexpr Form kForms[] = {{1, 1, 38}, {2, 1, 41}, {2, 2, 75}, {2, 4, 120}, {4, 4, 143}, {8, 4, 227}, {8, 8, 345}, {1, 4, 105}, {8, 16, 540}};
 
 template <int FLUSH>
 hipError_t by_shape(hb::LinearArgs &a, hipStream_t stream)
@@ -44,6 +47,7 @@ hipError_t by_shape(hb::LinearArgs &a, hipStream_t stream)
     uint64_t least = ~0ull;
     for (int i = 0; i < (int)(sizeof(kForms) / sizeof(kForms[0])); ++i) {
         const Form &f = kForms[i];
+        if (f.tiles == 16 && FLUSH != 128) continue;
         const uint64_t blocks = (a.rows + f.rows - 1) / f.rows * ((tiles + f.tiles - 1) / f.tiles), cost = (blocks + 255) / 256 * f.round;
         if (cost < least) least = cost, best = i;
     }
@@ -56,6 +60,9 @@ hipError_t by_shape(hb::LinearArgs &a, hipStream_t stream)
     case 4: return go<4, 1, 4, FLUSH == 32 ? 2 : 4, 1, FLUSH>(a, stream);
     case 5: return go<8, 1, 4, 2, 1, FLUSH>(a, stream);
     case 6: return go<8, 1, 8, 1, 1, FLUSH>(a, stream);
+    case 8:
+        if constexpr (FLUSH == 128) return go<8, 2, 8, 1, 1, FLUSH>(a, stream);
+        [[fallthrough]];
     default: return go<1, 1, FLUSH == 32 ? 1 : 4, FLUSH == 32 ? 16 : 4, FLUSH == 32 ? 1 : 4, FLUSH>(a, stream);
     }
 }

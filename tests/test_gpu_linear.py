@@ -47,6 +47,11 @@ def test_layers(inputs, outputs, group):
     _check(rng, 6, inputs, min(outputs, 520), group, 20)
 
 
+@pytest.mark.parametrize("rows,inputs,outputs,group", [(257, 130, 1100, 128), (300, 517, 1011, 256), (261, 33, 1025, 128)])
+def test_many_rows_and_outputs(rows, inputs, outputs, group):
+    _check(np.random.default_rng(rows + outputs), rows, inputs, outputs, group)
+
+
 @pytest.mark.parametrize("frac", [1, 7, 31])
 @pytest.mark.parametrize("rows,inputs,outputs,group", [(1, 517, 40, 32), (4, 640, 33, 128), (20, 256, 64, 64)])
 def test_any_number_of_the_ring(rows, inputs, outputs, group, frac):
