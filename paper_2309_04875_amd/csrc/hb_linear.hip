@@ -15,29 +15,30 @@ hipError_t go(hb::LinearArgs &a, hipStream_t stream)
     return hipGetLastError();
 }
 
-// Which form a layer takes: the one whose rounds of 256 workgroups, one for each compute unit, cost least.  More rows and tiles of outputs in a
-// workgroup use its digits and weights more often, and fewer fill the chip.  A round's time in tenths of a us, measured at 4096 inputs in
-// groups of 128; all of them grow alike with the inputs, and in groups of 32 to about 2.5 times as much.  us by form, for rows x (inputs ->
-// outputs), the form taken in brackets:
-//               rows, tiles a workgroup:   1, 1    2, 1    2, 2    2, 4    4, 4    8, 4    8, 8
-//    1 x (4096 -> 4096)                   [6.1]    7.1     8.9    12.7    14.3    21.2    32.3
-//    2 x                                   9.8    [7.9]    9.5    13.4    14.8    21.2    32.3
-//    4 x                                  16.7    11.8   [10.0]   13.7    16.1    21.6    32.9
-//    8 x                                  29.7    20.3    17.9   [14.6]   16.6    23.6    32.7
-//   16 x                                  56.8    35.0    32.7    26.5   [17.8]   24.3    33.5
-//   32 x                                   110    63.3    61.9    48.6    32.1   [25.4]   34.5
-//   64 x                                   219     122     122    94.9    59.2    48.1   [37.3]
-//   64 x (4096 -> 16384)                   886     494     503     384     240     187    [116]
-//    8 x (512 -> 512)                      3.8    [4.1]    3.9     3.9     4.9     6.3     8.0
-// Eight rows by sixteen tiles, with groups of 128, halve the digits to be made and read for each weight, at two wavefronts a SIMD for four: from two rounds of
-// the last on they are 4 to 11 % faster (64 x (4096 -> 16384) 109 for 113, 128 x (4096 -> 4096) 51 for 58, 512 x (1024 -> 2048) 37 for 41, but
-// 64 x (4096 -> 4096) 50 for 36).  Scaling every 64 or 32 inputs takes the registers of the second tile.
-// One row of many outputs (16384: 13.1 instead of 17.7) shares its digits among four tiles; up to 1024 inputs, four steps, it needs no sixteen
-// wavefronts (512 -> 1000 4.0 instead of 4.5).
+// Which form a layer takes: the one that costs least.  More rows and tiles of outputs in a workgroup use its digits and weights more often, and fewer fill
+// the chip.  A form's time is first + (rounds of 256 workgroups, one for each compute unit) x round, in tenths of a us as measured at 4096 inputs in groups
+// of 128; all of them grow alike with the inputs, and in groups of 32 to about twice as much.  us by form, for rows x (inputs -> outputs), the form taken
+// in brackets:
+//               rows, tiles a workgroup:   1, 1    2, 1    2, 2    2, 4    4, 4    4, 8    8, 8   8, 16
+//    1 x (4096 -> 4096)                   [6.0]    7.4     7.8     9.3    12.6    19.8    30.3    41.6
+//    2 x                                   9.8    [7.6]    8.1    10.0    12.8    19.8    30.4    41.7
+//    4 x                                  17.3    10.4    [8.4]   10.2    13.2    20.5    31.1    42.2
+//    8 x                                  31.4    17.3    14.4   [10.4]   13.2    20.4    32.1    43.2
+//   16 x                                  58.8    29.5    26.4    18.5   [13.6]   20.4    32.1    43.2
+//   32 x                                   115    53.4    50.4    34.9    24.8   [20.9]   32.3    43.5
+//   64 x                                   240     114     103    69.4    49.9   [32.9]   35.7    47.2
+//   16 x (4096 -> 16384)                   239     112     104    71.4    49.9   [34.0]   35.3    46.8
+//   64 x                                   967     452     413     280     197     121     104   [97.3]
+//   64 x, groups of 32                    1160     860     555     401     222     264    [217]
+//    8 x (512 -> 512)                     [3.6]    4.2     4.0     4.2     5.0     5.6     7.8    10.5
+// One row of many outputs (16384: 11.4 instead of 17.9) shares its digits among four tiles; up to 1024 inputs, four steps, it needs no sixteen
+// wavefronts (512 -> 1000 4.0 instead of 4.5).  Eight rows by sixteen tiles are for groups of 128: scaling every 64 or 32 inputs takes the registers of a
+// second tile.
 struct Form {
-    uint64_t rows, tiles, round;
+    uint64_t rows, tiles, first, round;
 };
-constexpr Form kForms[] = {{1, 1, 38}, {2, 1, 41}, {2, 2, 75}, {2, 4, 120}, {4, 4, 143}, {8, 4, 227}, {8, 8, 345}, {1, 4, 105}, {8, 16, 540}};
+constexpr Form kForms[] = {{1, 1, 23, 37}, {2, 1, 44, 31}, {2, 2, 24, 60}, {2, 4, 20, 83}, {4, 4, 13, 121}, {4, 8, 60, 143}, {8, 8, 125, 230},
+                           {1, 4, 44, 70}, {8, 16, 10, 480}};
 
 template <int FLUSH>
 hipError_t by_shape(hb::LinearArgs &a, hipStream_t stream)
@@ -48,7 +49,7 @@ hipError_t by_shape(hb::LinearArgs &a, hipStream_t stream)
     for (int i = 0; i < (int)(sizeof(kForms) / sizeof(kForms[0])); ++i) {
         const Form &f = kForms[i];
         if (f.tiles == 16 && FLUSH != 128) continue;
-        const uint64_t blocks = (a.rows + f.rows - 1) / f.rows * ((tiles + f.tiles - 1) / f.tiles), cost = (blocks + 255) / 256 * f.round;
+        const uint64_t blocks = (a.rows + f.rows - 1) / f.rows * ((tiles + f.tiles - 1) / f.tiles), cost = f.first + (blocks + 255) / 256 * f.round;
         if (cost < least) least = cost, best = i;
     }
     switch (best) {
@@ -56,9 +57,8 @@ hipError_t by_shape(hb::LinearArgs &a, hipStream_t stream)
     case 1: return go<2, 1, 1, 8, 1, FLUSH>(a, stream);
     case 2: return go<2, 1, 2, 8, 1, FLUSH>(a, stream);
     case 3: return go<2, 1, 4, 4, 2, FLUSH>(a, stream);
-    // (eight wavefronts where scaling every 32 inputs takes more registers than sixteen leave: 16 x (4096 -> 4096) 39 instead of 58)
-    case 4: return go<4, 1, 4, FLUSH == 32 ? 2 : 4, 1, FLUSH>(a, stream);
-    case 5: return go<8, 1, 4, 2, 1, FLUSH>(a, stream);
+    case 4: return go<4, 1, 4, FLUSH == 32 ? 2 : 4, 1, FLUSH>(a, stream);      // (scaling every 32 inputs takes more registers than sixteen wavefronts leave)
+    case 5: return go<4, 1, 8, 1, 2, FLUSH>(a, stream);
     case 6: return go<8, 1, 8, 1, 1, FLUSH>(a, stream);
     case 8:
         if constexpr (FLUSH == 128) return go<8, 2, 8, 1, 1, FLUSH>(a, stream);

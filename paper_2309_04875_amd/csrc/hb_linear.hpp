@@ -19,15 +19,16 @@ struct LinearArgs {
 
 constexpr uint32_t kDies = 8;
 constexpr int kLinearStep = 256;                     // inputs of a step
-constexpr int kLinearPlane = kLinearStep + 16;       // bytes of a digit's plane in LDS: rows of it fall into different banks
+constexpr int kPieceBytes = 16 * kLinearStep;        // one row's digits of a step in LDS: 16 planes of a byte an input, eight of each party
 
 typedef uint32_t u32x4_any_t __attribute__((ext_vector_type(4), aligned(1)));
-typedef uint32_t u32x2_any_t __attribute__((ext_vector_type(2), aligned(1)));
-typedef uint32_t u32_any_t __attribute__((aligned(1)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef uint64_t u64x2_any_t __attribute__((ext_vector_type(2), aligned(8)));
 
-// Digits of one row's inputs k0 .. k0 + 255 of both parties, 64 lanes at a time: lane l takes eight inputs of party l / 32.  In a plane (one digit
-// of one party) eight inputs lie as their even ones, then their odd ones: the order in which a weight's low and high four bits come.
+// Digits of one row's inputs k0 .. k0 + 255 of both parties, 64 lanes at a time: lane l takes eight inputs of party l / 32.  In a plane r (one digit
+// of one party) eight inputs lie as their even ones, then their odd ones: the order in which a weight's low and high four bits come.  Inputs 16 j .. 16 j + 15
+// of plane r are at 16 (16 j + (r xor j)), where no two lanes meet in a bank.
 // whole: all of them are there, for every lane (otherwise what is not there is a zero, and its place is read from elsewhere in the row).
 __device__ __forceinline__ void load_inputs(const LinearArgs &a, uint32_t row, uint32_t k0, uint32_t lane, bool whole, uint64_t (&v)[8])
 {
@@ -55,58 +56,54 @@ __device__ __forceinline__ void store_digits(uint8_t *planes, uint32_t lane, con
     uint32_t even[8], odd[8];
     digits_of({v[0], v[2], v[4], v[6]}, even);
     digits_of({v[1], v[3], v[5], v[7]}, odd);
-    uint8_t *to = planes + (lane / 32 * 8) * kLinearPlane + 8 * (lane % 32);
+    const uint32_t j = lane % 32 / 2, to = 256 * j + 16 * ((lane / 32 * 8) ^ j) + 8 * (lane % 2);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) *reinterpret_cast<uint64_t *>(to + i * kLinearPlane) = ((uint64_t)odd[i] << 32) | even[i];
+    for (int i = 0; i < 8; ++i) *reinterpret_cast<uint64_t *>(planes + (to ^ (16 * i))) = ((uint64_t)odd[i] << 32) | even[i];
 }
 
-// Half a step's weights of one lane, 16 bytes of row n = lane mod 16 of a tile: 32 inputs.  FLUSH, the inputs that go into one sum before it is scaled
-// (what divides the group): of 128 and 64 inputs lane quarter q holds 16 for one matrix instruction, of 32 eight.
-struct HalfWeights {
-    uint32_t w[4];
+// A step's weights of a tile, 16 rows of 128 bytes: lane l loads 16 bytes l mod 8 of rows l / 8 and l / 8 + 8, and they go through LDS to where the matrix
+// instruction takes them.  (Loaded from there at once, 16 rows by 64 bytes an instruction, 16 cache lines are asked for in each quarter of it:
+// 64 x (4096 -> 16384) 97 us for 109, 1 x (4096 -> 4096) 5.0 for 5.5, 64 x (4096 -> 16384) in groups of 32 217 for 339.)
+struct StepWeights {
+    u32x4_t w[2];
 };
-template <int FLUSH>
-__device__ __forceinline__ uint32_t piece_offset(uint32_t piece, uint32_t q)
+// In LDS bytes 16 p .. of row r lie at 128 r + 16 (p xor r mod 8): no two lanes meet in a bank.
+__device__ __forceinline__ void store_weights(uint8_t *tile, uint32_t lane, const StepWeights &s)
 {
-    if (FLUSH == 128) return 16 * q;                         // one piece of 16 bytes
-    if (FLUSH == 64) return 32 * piece + 8 * q;              // two of 8
-    return 16 * piece + 4 * q;                               // four of 4
-}
-// p: the half's first byte of a lane's output.
-template <int FLUSH>
-__device__ __forceinline__ void load_weights(const uint8_t *p, uint32_t q, HalfWeights &s)
-{
-    constexpr int kPieces = 128 / FLUSH, kWords = 4 / kPieces;
+    const uint32_t row = lane / 8;
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-        const uint8_t *from = p + piece_offset<FLUSH>(i, q);
-        if constexpr (kWords == 4) {
-            const u32x4_any_t v = *reinterpret_cast<const u32x4_any_t *>(from);
-            s.w[0] = v.x, s.w[1] = v.y, s.w[2] = v.z, s.w[3] = v.w;
-        } else if constexpr (kWords == 2) {
-            const u32x2_any_t v = *reinterpret_cast<const u32x2_any_t *>(from);
-            s.w[2 * i] = v.x, s.w[2 * i + 1] = v.y;
-        } else {
-            s.w[i] = *reinterpret_cast<const u32_any_t *>(from);
-        }
+    for (int i = 0; i < 2; ++i) *reinterpret_cast<u32x4_t *>(tile + 128 * (8 * i + row) + 16 * (lane % 8 ^ row)) = s.w[i];
+}
+// The same from memory a byte at a time, where bytes of some lane lie behind the last row: the last one instead, for no input has them.
+__device__ __forceinline__ void store_weights_end(uint8_t *tile, uint32_t lane, const uint8_t *p, uint32_t eight_rows, const uint8_t *last)
+{
+    const uint32_t row = lane / 8;
+#pragma unroll 8
+    for (uint32_t j = 0; j < 32; ++j) {
+        const uint8_t *from = p + (j / 16 != 0 ? eight_rows : 0) + j % 16;
+        tile[128 * (8 * (j / 16) + row) + 16 * (lane % 8 ^ row) + j % 16] = *(from < last ? from : last);
     }
 }
-// The same a byte at a time where bytes of some lane lie behind the last row: the last one instead, for no input has them.  A word after the other: what
-// this rare path would hold at once would be taken from the loop's registers.
+// Half a step's weights of one lane, row n = lane mod 16: 32 inputs.  FLUSH, the inputs that go into one sum before it is scaled (what divides the group): of
+// 128 and 64 inputs lane quarter q takes 16 for one matrix instruction, of 32 eight.
 template <int FLUSH>
-__device__ __forceinline__ void load_weights_end(const uint8_t *p, uint32_t q, const uint8_t *last, HalfWeights &s)
+__device__ __forceinline__ void half_weights(const uint8_t *tile, uint32_t lane, int half, uint32_t (&w)[4])
 {
-    constexpr int kWords = FLUSH / 32;
+    const uint32_t q = lane / 16;
+    const uint8_t *row = tile + lane % 16 * 128;
+    auto at = [&](uint32_t p) { return row + 16 * (p ^ lane % 8); };
+    if constexpr (FLUSH == 128) {
+        const u32x4_t v = *reinterpret_cast<const u32x4_t *>(at(4 * half + q));
+        w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+    } else if constexpr (FLUSH == 64) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint8_t *word = p + piece_offset<FLUSH>(i / kWords, q) + 4 * (i % kWords);
-        uint32_t v = 0;
-        for (int j = 3; j >= 0; --j) {
-            const uint8_t *from = word + j;
-            v = v << 8 | *(from < last ? from : last);
+        for (int i = 0; i < 2; ++i) {
+            const u32x2_t v = *reinterpret_cast<const u32x2_t *>(at(4 * half + 2 * i + q / 2) + 8 * (q % 2));
+            w[2 * i] = v.x, w[2 * i + 1] = v.y;
         }
-        s.w[i] = v;
-        __builtin_amdgcn_sched_barrier(0);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const uint32_t *>(at(4 * half + i) + 4 * q);
     }
 }
 // 16 q of the even inputs, then of the odd ones.
@@ -127,15 +124,15 @@ __device__ __forceinline__ void unpack_weights(uint32_t w, int &even, int &odd)
 // A workgroup goes through the inputs in blocks of WK * P steps, whose digits its wavefronts make together and all of them read (with
 // WN = P = 1 each makes its own); wavefront (wn, wk) multiplies steps wk, wk + WK, .. of a block with its own RT tiles.
 template <int TM, int RT, int WN, int WK, int P, int FLUSH>
-__global__ void __launch_bounds__(64 * WN * WK, 2)
+__global__ void __launch_bounds__(64 * WN * WK, (TM * RT <= 8 && WK == 1 && FLUSH != 32 ? 4 : 2))
 linear_q4_kernel(LinearArgs a)
 {
     constexpr int kWaves = WN * WK, kSteps = WK * P, kOwn = kSteps * TM / kWaves;      // kOwn: pieces of digits that a wavefront makes
     static_assert(kOwn * kWaves == kSteps * TM, "every wavefront makes as many pieces");
     constexpr bool kShared = WN > 1 || P > 1;
-    constexpr int kDigitBytes = 16 * kLinearPlane, kBlockBytes = kSteps * TM * kDigitBytes, kBuffers = kShared && kBlockBytes <= 72 * 1024 ? 2 : 1;
+    constexpr int kBlockBytes = kSteps * TM * kPieceBytes, kBuffers = kShared && 2 * kBlockBytes + kWaves * RT * 2048 <= 160 * 1024 ? 2 : 1;
     static_assert(kWaves * RT * TM * 256 <= kBuffers * kBlockBytes, "the sums' exchange takes the digits' place");
-    __shared__ __align__(16) uint8_t lds[kBuffers * kBlockBytes];
+    __shared__ __align__(256) uint8_t lds[kBuffers * kBlockBytes + kWaves * RT * 2048];
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint32_t q = lane / 16, wn = wave % WN, wk = wave / WN;
     // Workgroups with the same weights run on the same die (they are dealt out to the eight in turn), whose cache then reads them once.
@@ -145,20 +142,24 @@ linear_q4_kernel(LinearArgs a)
     const uint32_t steps = (a.in + kLinearStep - 1) / kLinearStep;
     // A lane's rows of weights and scales; outputs behind the last are the last.
     const uint8_t *weight_row[RT];
+    uint32_t eight_rows[RT];                                  // bytes from a lane's first row of weights to its second
     const int32_t *scale_row[RT];
     const uint32_t row_bytes = (a.in + 1) / 2;
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-        const uint32_t out = 16 * (tile0 + t) + lane % 16, n = out < a.outs ? out : a.outs - 1;
-        weight_row[t] = a.weight + (uint64_t)n * row_bytes;
-        scale_row[t] = a.scales + (uint64_t)n * a.groups;
+        auto row = [&](uint32_t n) { return 16 * (tile0 + t) + n < a.outs ? 16 * (tile0 + t) + n : a.outs - 1; };
+        weight_row[t] = a.weight + (uint64_t)row(lane / 8) * row_bytes + 16 * (lane % 8);
+        eight_rows[t] = (row(lane / 8 + 8) - row(lane / 8)) * row_bytes;
+        scale_row[t] = a.scales + (uint64_t)row(lane % 16) * a.groups;
     }
+    uint8_t *my_weights = lds + kBuffers * kBlockBytes + wave * (RT * 2048);
     const uint32_t last_out = 16 * (tile0 + RT) < a.outs ? 16 * (tile0 + RT) - 1 : a.outs - 1;
     const uint64_t last_row = (uint64_t)last_out * row_bytes;
     int64_t sum[TM][RT][2] = {};
-    constexpr int kScales = 128 / FLUSH;
-    HalfWeights weights[P][2][RT];
-    int32_t scales[P][2][RT][kScales];
+    // Scales: lane quarter q loads that of the q-th FLUSH inputs of every four in a step.
+    constexpr int kScales = 128 / FLUSH, kScaleLoads = FLUSH == 32 ? 2 : 1;
+    StepWeights weights[P][RT];
+    int32_t scales[P][RT][kScaleLoads];
     uint64_t inputs[kOwn][8];
     auto load_rows = [&](uint32_t first) {                    // of the block that begins with step `first`
 #pragma unroll
@@ -167,38 +168,41 @@ linear_q4_kernel(LinearArgs a)
             if (step < steps) load_inputs(a, row, kLinearStep * step, lane, kLinearStep * (step + 1) <= a.in && row < a.rows, inputs[i]);
         }
     };
-    auto load_half = [&](uint32_t step, int p, int half) {
-        const uint32_t k = kLinearStep * step + 128 * half;
-        if (last_row + k / 2 + 64 <= a.weight_bytes) {
+    // whether no weight of the step lies behind the last row
+    auto weights_there = [&](uint32_t step) { return last_row + kLinearStep * step / 2 + 128 <= a.weight_bytes; };
+    auto load_step = [&](uint32_t step, int p) {
+        const uint32_t k = kLinearStep * step;
+        if (weights_there(step)) {
 #pragma unroll
-            for (int t = 0; t < RT; ++t) load_weights<FLUSH>(weight_row[t] + k / 2, q, weights[p][half][t]);
-        } else {
-#pragma unroll
-            for (int t = 0; t < RT; ++t) load_weights_end<FLUSH>(weight_row[t] + k / 2, q, a.weight + a.weight_bytes - 1, weights[p][half][t]);
+            for (int t = 0; t < RT; ++t) {
+                const uint8_t *from = weight_row[t] + k / 2;
+                weights[p][t].w[0] = *reinterpret_cast<const u32x4_any_t *>(from);
+                weights[p][t].w[1] = *reinterpret_cast<const u32x4_any_t *>(from + eight_rows[t]);
+            }
         }
 #pragma unroll
-        for (int f = 0; f < kScales; ++f) {
-            uint32_t group = (uint32_t)(((k + FLUSH * f) * a.group_inverse) >> 40);
+        for (int i = 0; i < kScaleLoads; ++i) {
+            const uint32_t piece = FLUSH == 128 ? q % 2 : q + 4 * i;
+            uint32_t group = (uint32_t)(((k + FLUSH * piece) * a.group_inverse) >> 40);
             group = group < a.groups ? group : a.groups - 1;
 #pragma unroll
-            for (int t = 0; t < RT; ++t) scales[p][half][t][f] = scale_row[t][group];
+            for (int t = 0; t < RT; ++t) scales[p][t][i] = scale_row[t][group];
         }
     };
     load_rows(0);
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        if (p * WK + wk < steps) {
-            load_half(p * WK + wk, p, 0);
-            load_half(p * WK + wk, p, 1);
-        }
+        if (p * WK + wk < steps) load_step(p * WK + wk, p);
     }
     uint32_t buffer = 0;
     for (uint32_t first = 0; first < steps; first += kSteps) {
         uint8_t *block = lds + buffer * kBlockBytes;
+        uint32_t l = lane;
+        if constexpr (kWaves == 16) settle(l);                // (what follows from it would be kept in registers, of which sixteen wavefronts have 128)
 #pragma unroll
         for (int i = 0; i < kOwn; ++i) {
             const uint32_t piece = wave * kOwn + i;
-            if (first + piece / TM < steps) store_digits(block + piece * kDigitBytes, lane, inputs[i]);
+            if (first + piece / TM < steps) store_digits(block + piece * kPieceBytes, l, inputs[i]);
         }
         load_rows(first + kSteps);
         if constexpr (kShared) __syncthreads();
@@ -208,19 +212,35 @@ linear_q4_kernel(LinearArgs a)
         for (int p = 0; p < P; ++p) {
             const uint32_t step = first + p * WK + wk;
             if (step >= steps) break;
-            const uint8_t *column = block + (p * WK + wk) * (TM * kDigitBytes) + (lane % 16) * kLinearPlane;
+            int32_t now[RT][kScaleLoads];
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                if (weights_there(step)) store_weights(my_weights + 2048 * t, l, weights[p][t]);
+                else store_weights_end(my_weights + 2048 * t, lane, weight_row[t] + kLinearStep * step / 2, eight_rows[t], a.weight + a.weight_bytes - 1);
+#pragma unroll
+                for (int i = 0; i < kScaleLoads; ++i) now[t][i] = scales[p][t][i];
+            }
+            wave_exchange();
+            if (step + kSteps < steps) load_step(step + kSteps, p);
+            // inputs 16 j .. of this lane's digit, j = c + what lane quarter q adds
+            const uint8_t *digits_here = block + (p * WK + wk) * (TM * kPieceBytes);
+            const uint32_t of_q = FLUSH == 128 ? 2 * q : FLUSH == 64 ? q : q / 2, lane_at = 256 * of_q + 16 * (lane % 16 ^ of_q);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 int w[RT][8];
                 int32_t scale[RT][kScales];
 #pragma unroll
                 for (int t = 0; t < RT; ++t) {
+                    uint32_t packed[4];
+                    half_weights<FLUSH>(my_weights + 2048 * t, l, half, packed);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) unpack_weights(weights[p][half][t].w[i], w[t][2 * i], w[t][2 * i + 1]);
+                    for (int i = 0; i < 4; ++i) unpack_weights(packed[i], w[t][2 * i], w[t][2 * i + 1]);
 #pragma unroll
-                    for (int f = 0; f < kScales; ++f) scale[t][f] = scales[p][half][t][f];
+                    for (int f = 0; f < kScales; ++f) {
+                        const int piece = kScales * half + f;
+                        scale[t][f] = __builtin_amdgcn_ds_bpermute(4 * (16 * (piece % 4) + l % 16), now[t][piece / 4]);
+                    }
                 }
-                if (step + kSteps < steps) load_half(step + kSteps, p, half);
 #pragma unroll
                 for (int f = 0; f < kScales; ++f) {
                     // A row's sums are scaled while the next one's are under way.
@@ -236,17 +256,17 @@ linear_q4_kernel(LinearArgs a)
                     };
 #pragma unroll
                     for (int m = 0; m < TM; ++m) {
-                        const uint8_t *row = column + m * kDigitBytes + 128 * half;
+                        auto digits_at = [&](uint32_t c) { return digits_here + m * kPieceBytes + (lane_at ^ (16 * c)) + 256 * c; };
                         const i32x4_t zero{0, 0, 0, 0};
                         if constexpr (FLUSH == 32) {
-                            const i32x2_t digits = *reinterpret_cast<const i32x2_t *>(row + 32 * f + 8 * q);
+                            const i32x2_t digits = *reinterpret_cast<const i32x2_t *>(digits_at(8 * half + 2 * f) + 8 * (q % 2));
 #pragma unroll
                             for (int t = 0; t < RT; ++t) part[m % 2][t] = mfma_16x16x32(digits, i32x2_t{w[t][2 * f], w[t][2 * f + 1]}, zero);
                         } else {
 #pragma unroll
                             for (int h = 0; h < FLUSH / 64; ++h) {
                                 const int at = FLUSH == 128 ? h : f;
-                                const i32x4_t digits = *reinterpret_cast<const i32x4_t *>(row + (FLUSH == 128 ? 32 * q + 16 * h : 64 * f + 16 * q));
+                                const i32x4_t digits = *reinterpret_cast<const i32x4_t *>(digits_at(8 * half + (FLUSH == 128 ? h : 4 * f)));
 #pragma unroll
                                 for (int t = 0; t < RT; ++t)
                                     part[m % 2][t] = mfma_16x16x64(digits, i32x4_t{w[t][4 * at], w[t][4 * at + 1], w[t][4 * at + 2], w[t][4 * at + 3]},
