@@ -185,13 +185,14 @@ struct Planes {
         }
     }
 
+    typedef Flipped<4> Numbers4;
     typedef uint32_t Digits[8][4];            // otherwise: a lane's 16 numbers of a row: digit, four numbers a word
 
     static __device__ __forceinline__ i32x4_t operand(const uint8_t *at) { return *reinterpret_cast<const i32x4_t *>(at); }
     // sums += numbers 4 s .. 4 s + 3 (bytes flipped) of one matrix times its vectors.
-    static __device__ __forceinline__ void multiply(i32x4_t (&sums)[GT], uint64_t z0, uint64_t z1, uint64_t z2, uint64_t z3, int s, const Column &column)
+    static __device__ __forceinline__ void multiply(i32x4_t (&sums)[GT], const Numbers4 &z, int s, const Column &column)
     {
-        const i32x4_t low{(int)z0, (int)z1, (int)z2, (int)z3}, high{(int)(z0 >> 32), (int)(z1 >> 32), (int)(z2 >> 32), (int)(z3 >> 32)};
+        const i32x4_t low{(int)z.low[0], (int)z.low[1], (int)z.low[2], (int)z.low[3]}, high{(int)z.high[0], (int)z.high[1], (int)z.high[2], (int)z.high[3]};
         i32x4_t right[GT];
 #pragma unroll
         for (int tile = 0; tile < GT; ++tile) {
@@ -219,30 +220,34 @@ struct Planes {
             }
         }
     }
-    static __device__ __forceinline__ void digits_at(Digits &d, int s, uint64_t z0, uint64_t z1, uint64_t z2, uint64_t z3)
+    static __device__ __forceinline__ void digits_at(Digits &d, int s, const Numbers4 &z)
     {
         uint32_t w[8];
-        digits_of_flipped({z0, z1, z2, z3}, w);
+        turn_bytes(z.low, w);
+        turn_bytes(z.high, w + 4);
 #pragma unroll
         for (int i = 0; i < 8; ++i) d[i][s] = w[i];
     }
 
-    // sums += the three matrices, 16 numbers a lane each, times their vectors: numbers(x) loads D, state(p, j) is that of the word for number j of b_p.
+    // sums += the three matrices, 16 numbers a lane each, times their vectors: numbers(x) loads D, state(start, j) is that of the word for number j of b_p, start being start_of(p).
     // Words are drawn eight in step (four: 1 to 4 % slower; 16: as fast).  The loads are under way while words are drawn, but for GT = 8, where the
     // 32 registers that they hold would be the fifth wavefront's on a SIMD.
-    template <class Numbers, class State>
-    static __device__ __forceinline__ void multiply_three(i32x4_t (&sums)[GT], const Column &column, const Numbers &numbers, const State &state)
+    template <class Numbers, class Start, class State>
+    static __device__ __forceinline__ void multiply_three(i32x4_t (&sums)[GT], const Column &column, const Numbers &numbers, const Start &start_of, const State &state)
     {
         uint64_t delta[16];
         Digits d;
         auto masked = [&] {
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
-                uint64_t z[4];
+                Numbers4 z;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) z[j] = delta[4 * s + j] ^ kDigitBias;
-                if constexpr (WHOLE) multiply(sums, z[0], z[1], z[2], z[3], s, column + 2 * matrix);
-                else digits_at(d, s, z[0], z[1], z[2], z[3]);
+                for (int j = 0; j < 4; ++j) {
+                    z.low[j] = (uint32_t)delta[4 * s + j] ^ kDigitFlip;
+                    z.high[j] = (uint32_t)(delta[4 * s + j] >> 32) ^ kDigitFlip;
+                }
+                if constexpr (WHOLE) multiply(sums, z, s, column + 2 * matrix);
+                else digits_at(d, s, z);
             }
             if constexpr (!WHOLE) multiply(sums, d, column + 2 * matrix);
         };
@@ -253,16 +258,25 @@ struct Planes {
         }
 #pragma unroll 1
         for (int p = 0; p < 2; ++p) {
+            uint64_t start = start_of(p);
+            settle(start);                                    // (else p gamma is a product for every word)
 #pragma unroll
             for (int s = 0; s < 4; s += 2) {
                 uint64_t z[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) z[j] = state(p, 4 * s + j);
-                mix_flipped<true>(z);
+                for (int j = 0; j < 8; ++j) z[j] = state(start, 4 * s + j);
+                Flipped<8> words;
+                mix_flipped<true>(z, words);
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    if constexpr (WHOLE) multiply(sums, z[4 * x], z[4 * x + 1], z[4 * x + 2], z[4 * x + 3], s + x, column + p * matrix);
-                    else digits_at(d, s + x, z[4 * x], z[4 * x + 1], z[4 * x + 2], z[4 * x + 3]);
+                    Numbers4 four;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        four.low[j] = words.low[4 * x + j];
+                        four.high[j] = words.high[4 * x + j];
+                    }
+                    if constexpr (WHOLE) multiply(sums, four, s + x, column + p * matrix);
+                    else digits_at(d, s + x, four);
                 }
             }
             if constexpr (!WHOLE) multiply(sums, d, column + p * matrix);
@@ -416,8 +430,9 @@ attention_scores_kernel(AttentionArgs a)
                     delta[2 * j + 1] = v.b;
                 }
             };
-            auto state = [&](int p, int j) { return z0 + (uint64_t)(2 * (8 * (j / 2) + j % 2) + p) * kGamma; };
-            P::multiply_three(sums, at, numbers, state);
+            auto start_of = [&](int p) { return p == 0 ? z0 : z0 + kGamma; };
+            auto state = [&](uint64_t start, int j) { return start + (uint64_t)(2 * (8 * (j / 2) + j % 2)) * kGamma; };
+            P::multiply_three(sums, at, numbers, start_of, state);
             z0 += 128 * kGamma;
             at = at + P::per_64;
         }
@@ -499,8 +514,9 @@ attention_values_kernel(AttentionArgs a)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) delta[j] = load_stream(c.values + row_at[64 * block + 16 * g + j] + dim);
             };
-            auto state = [&](int p, int j) { return row_state[64 * block + 16 * g + j] + (z + (uint64_t)p * kGamma); };
-            P::multiply_three(sums, column + P::per_64 * block, numbers, state);
+            auto start_of = [&](int p) { return p == 0 ? z : z + kGamma; };
+            auto state = [&](uint64_t start, int j) { return row_state[64 * block + 16 * g + j] + start; };
+            P::multiply_three(sums, column + P::per_64 * block, numbers, start_of, state);
         }
         __syncthreads();
     }

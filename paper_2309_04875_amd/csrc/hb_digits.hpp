@@ -26,23 +26,24 @@ __device__ __forceinline__ void turn_bytes(const uint32_t (&w)[4], uint32_t *out
     out[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
 }
 
-// Digits of four words whose bytes have their top bits flipped already, of v - 0x8080808080808080 that is: one addition less for each number
-// where sums of such digits with a vector are owed 0x8080808080808080 times the vector's sum, once for all of them.
-__device__ __forceinline__ void digits_of_flipped(const uint64_t (&v)[4], uint32_t (&out)[8])
-{
-    const uint32_t low[4] = {(uint32_t)v[0], (uint32_t)v[1], (uint32_t)v[2], (uint32_t)v[3]};
-    const uint32_t high[4] = {(uint32_t)(v[0] >> 32), (uint32_t)(v[1] >> 32), (uint32_t)(v[2] >> 32), (uint32_t)(v[3] >> 32)};
-    turn_bytes(low, out);
-    turn_bytes(high, out + 4);
-}
+// Numbers in halves, the bytes' top bits flipped: x - 0x8080808080808080 in digits, one addition less for each number where sums of such digits with a
+// vector are owed 0x8080808080808080 times the vector's sum, once for all of them.
+template <int N>
+struct Flipped {
+    uint32_t low[N], high[N];
+};
 
-// Dealer words of N states with the top bits of their bytes flipped; the last xor of the generator takes the flip along.
+// Dealer words of N states, flipped: the last xor of the generator takes the flip along.  (Halves, for a register each: as 64-bit numbers they would be moved to
+// where four of a half lie side by side, an instruction and a half a word.)
 template <bool RUNS, int N>
-__device__ __forceinline__ void mix_flipped(uint64_t (&z)[N])
+__device__ __forceinline__ void mix_flipped(uint64_t (&z)[N], Flipped<N> &out)
 {
     auto last = [&](uint64_t (&t)[N]) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) z[i] = bitop3<kTtXor3>(z[i], t[i], kDigitBias);
+        for (int i = 0; i < N; ++i) {
+            out.low[i] = bitop3<kTtXor3>((uint32_t)z[i], (uint32_t)t[i], kDigitFlip);
+            out.high[i] = bitop3<kTtXor3>((uint32_t)(z[i] >> 32), (uint32_t)(t[i] >> 32), kDigitFlip);
+        }
     };
     uint64_t t[N];
     if constexpr (RUNS) {                                      // as in mix_words
@@ -63,7 +64,8 @@ __device__ __forceinline__ void mix_flipped(uint64_t (&z)[N])
         settle(t);
         priority<true, kXorRuns>();
         last(t);
-        settle(z);
+        settle(out.low);
+        settle(out.high);
         priority<true, kElsewhere>();
     } else {
 #pragma unroll
