@@ -488,25 +488,56 @@ attention_values_kernel(AttentionArgs a)
     const uint64_t z = (uint64_t)(2 * dim) * kGamma;
     const QuadTurn turn(lane);
     i32x4_t sums[GT] = {};
+    // What a thread needs for the next chunk's vectors is under way while this one's are multiplied: the weight's shares, the position's page, that page's
+    // seed, and the page of the chunk after it.  (For GT = 8 there are no registers for that.)
+    constexpr bool kEarly = GT < 8;
+    const uint32_t my_place = threadIdx.x % CHUNK;            // the place in the chunk of every number that this thread makes
+    int32_t page = -1, next_page = -1;
+    uint64_t p0 = 0, p1 = 0, seed = 0;
+    auto find = [&](uint32_t t0) { return (int32_t)page_of(a, piece.b, t0 + my_place, end); };
+    auto weight_at = [&](uint32_t i, uint32_t t0) {
+        const bool asked = i / CHUNK < h.count && t0 + my_place < end;
+        return (row0 + (asked ? i / CHUNK : 0)) * a.max_len + (asked ? t0 + my_place : first);
+    };
+    auto load_weight = [&](uint32_t i, uint32_t t0) {
+        const uint64_t n = weight_at(i, t0);
+        p0 = a.scores[0][n];
+        p1 = a.scores[1][n];
+    };
+    auto load_seed = [&] {
+        if (threadIdx.x < CHUNK && page >= 0) seed = c.page_seeds[page];
+    };
+    page = find(first);
+    if constexpr (kEarly) {
+        load_weight(threadIdx.x, first);
+        next_page = find(first + CHUNK);
+    }
+    load_seed();
     for (uint32_t t0 = first; t0 < end; t0 += CHUNK) {
         uint32_t thread = threadIdx.x;
         settle(thread);                                       // what follows from it is not kept in registers from chunk to chunk
 #pragma unroll 1
         for (uint32_t i = thread; i < GT * CHUNK; i += threads) {
-            const uint32_t head = i / CHUNK, t = t0 + i % CHUNK;
-            const bool asked = head < h.count && t < end;
-            const uint64_t n = (row0 + (asked ? head : 0)) * a.max_len + (asked ? t : first);
-            const uint64_t p0 = a.scores[0][n], p1 = a.scores[1][n];
-            const bool there = page_of(a, piece.b, t, end) >= 0 && asked;
-            const uint64_t s = state_of(a.seed_p, 2 * n), a0 = there ? mix64(s) : 0, a1 = there ? mix64(s + kGamma) : 0;
+            if (!kEarly || i >= threads) load_weight(i, t0);
+            const bool there = page >= 0 && i / CHUNK < h.count;
+            const uint64_t s = state_of(a.seed_p, 2 * weight_at(i, t0)), a0 = there ? mix64(s) : 0, a1 = there ? mix64(s + kGamma) : 0;
             const uint64_t eps = there ? (p0 - a0) + (p1 - a1) : 0;                        // opened
-            P::store_vectors(lds, turn, i % CHUNK, head, eps, a0, a1, owed);
+            P::store_vectors(lds, turn, i % CHUNK, i / CHUNK, eps, a0, a1, owed);
         }
-        for (uint32_t i = thread; i < CHUNK; i += threads) {
-            const int64_t page = page_of(a, piece.b, t0 + i, end);
-            const uint64_t place = place_in_page(c, h.head, (t0 + i) % c.page, 0);
-            row_at[i] = page >= 0 ? page * page_numbers(c) + place : 0;       // without a value: the first one's, times zeros
-            row_state[i] = page >= 0 ? state_of(stream_word(c.page_seeds[page], 1), 2 * place) : 0;
+        if (thread < CHUNK) {
+            const uint64_t place = place_in_page(c, h.head, (t0 + thread) % c.page, 0);
+            row_at[thread] = page >= 0 ? page * page_numbers(c) + place : 0;  // without a value: the first one's, times zeros
+            row_state[thread] = page >= 0 ? state_of(stream_word(seed, 1), 2 * place) : 0;
+        }
+        if (t0 + CHUNK < end) {
+            if constexpr (kEarly) {
+                page = next_page;
+                load_weight(thread, t0 + CHUNK);
+                next_page = find(t0 + 2 * CHUNK);
+            } else {
+                page = find(t0 + CHUNK);
+            }
+            load_seed();
         }
         __syncthreads();
         for (uint32_t block = 0; block < CHUNK / 64 && t0 + 64 * block < end && c.pages != 0 && dim0 < c.dim; ++block) {
