@@ -113,7 +113,7 @@ constexpr int kAttentionBlock = 512, kAttentionWaves = kAttentionBlock / 64, kJo
 // Two forms.  WHOLE: a left operand is the lower (or upper) halves of four numbers as they are, four digits each, and a column holds for a number the
 // digits s, s-1, s-2, s-3 of its vector (for the upper halves s-4 ..: the columns of weight 2^(8(s-4))), zeros below digit 0: planes [s][v] of four
 // bytes a place.  Otherwise digit i of 16 numbers is an operand, their bytes turned before (12 instructions a number of the cache and its two
-// masks, of 61), and a column holds digit s - i: planes [digit][v] of a byte a place, the columns of digit i being the planes 2 GT i further up,
+// masks, of 51), and a column holds digit s - i: planes [digit][v] of a byte a place, the columns of digit i being the planes 2 GT i further up,
 // planes of zeros before the first, and tiles whose columns all have s < i left out.  WHOLE has fewer instructions, but four times the planes to
 // write and to hold: it is for one or two heads at a time (32 heads of 4096 positions of 128, one query head each, 85 -> 78 us; 8192 of 8 heads 53 -> 49; eight
 // sequences of none to 4096 with two 126 -> 117) and, 64 positions at a time, for the values of four (2 x 4096 of 192 110 -> 104, 4 x 1000 of 128 40 -> 39; their
@@ -229,11 +229,13 @@ struct Planes {
         for (int i = 0; i < 8; ++i) d[i][s] = w[i];
     }
 
-    // sums += the three matrices, 16 numbers a lane each, times their vectors: numbers(x) loads D, state(start, j) is that of the word for number j of b_p, start being start_of(p).
+    // sums += the three matrices, 16 numbers a lane each, times their vectors: numbers(x) loads D, state(start, j), start being start_of(p), is that of the
+    // word for number j of b_p.
     // Words are drawn eight in step (four: 1 to 4 % slower; 16: as fast).  The loads are under way while words are drawn, but for GT = 8, where the
     // 32 registers that they hold would be the fifth wavefront's on a SIMD.
     template <class Numbers, class Start, class State>
-    static __device__ __forceinline__ void multiply_three(i32x4_t (&sums)[GT], const Column &column, const Numbers &numbers, const Start &start_of, const State &state)
+    static __device__ __forceinline__ void multiply_three(i32x4_t (&sums)[GT], const Column &column, const Numbers &numbers, const Start &start_of,
+                                                          const State &state)
     {
         uint64_t delta[16];
         Digits d;

@@ -37,10 +37,9 @@ constexpr int kAppendBlock = 256;
 // What bounds it: HBM (24 bytes a key or value, 32 a query), and beside it vector-ALU issue: a rotated number takes four dealer words for its
 // truncation, and every number of the cache two for its mask, 18 instructions each.  A thread takes N neighbours (dimensions d ..) and the N that
 // turn with them (d + rot/2 ..; the next N elsewhere), so that both multiply the same row of the tables and a number's words are drawn in step;
-// N = 2 (16-byte accesses, half the addresses) where the rotated part and the rest divide into such groups: 2048 tokens of 8 + 8 + 32
-// heads of 128, 370 MB, in 76 us (4.9 TB/s) instead of 80.  Keys, values and queries have workgroups of their own, whose wavefronts then do the same.  The groups of a token are
-// shared out to workgroups, or
-// several tokens with few share one.
+// N = 2 (16-byte accesses, half the addresses) where the rotated part and the rest divide into such groups: 2048 tokens of 8 + 8 + 32 heads of 128,
+// 370 MB, in 76 us (4.9 TB/s) instead of 80.  Keys, values and queries have workgroups of their own, whose wavefronts then do the same.  The groups
+// of a token are shared out to workgroups, or several tokens with few share one.
 struct AppendShape {
     uint32_t blocks;            // of this kind (keys, values or queries)
     uint32_t groups;            // of 2 N numbers of a token

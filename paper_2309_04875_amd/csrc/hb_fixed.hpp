@@ -40,12 +40,4 @@ __device__ __forceinline__ Pair truncate_drawn(Pair y, int f, uint64_t z)
 // State of word j of the generator started at s: mix64 of it is the word.
 __device__ __forceinline__ uint64_t state_of(uint64_t s, uint64_t j) { return s + (j + 1) * kGamma; }
 
-// Sum of v over the wavefront, in every lane.
-__device__ __forceinline__ uint64_t wave_sum(uint64_t v)
-{
-#pragma unroll
-    for (int step = 32; step > 0; step >>= 1) v += __shfl_xor((unsigned long long)v, step, 64);
-    return v;
-}
-
 }  // namespace hb

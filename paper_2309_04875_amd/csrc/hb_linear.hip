@@ -10,7 +10,7 @@ hipError_t go(hb::LinearArgs &a, hipStream_t stream)
     const uint64_t tiles = ((uint64_t)a.outs + 16 * WN * RT - 1) / (16 * WN * RT);
     a.row_tiles = (a.rows + TM - 1) / TM;
     const uint64_t blocks = (tiles + hb::kDies - 1) / hb::kDies * hb::kDies * a.row_tiles;
-    if (blocks > 0x7fffffffull) return hipErrorInvalidConfiguration;
+    if (blocks > 0xffffffffull / (64 * WN * WK)) return hipErrorInvalidConfiguration;     // a grid has fewer than 2^32 threads
     hipLaunchKernelGGL((hb::linear_q4_kernel<TM, RT, WN, WK, P, FLUSH>), dim3((unsigned)blocks), dim3(64 * WN * WK), 0, stream, a);
     return hipGetLastError();
 }
