@@ -296,6 +296,7 @@ __device__ __forceinline__ void join_digits(const i32x4_t (&sums)[GT], uint32_t 
     uint64_t weight = 1;
 #pragma unroll
     for (int s = 1; s < kPer; ++s) weight = lane % 16 / (2 * GT) == s ? 1ull << (8 * s) : weight;
+    if constexpr (kPer > 1) settle(weight);             // (the product does not become a shift by an amount in a vector register)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         uint64_t y = 0;
