@@ -29,16 +29,15 @@ hipError_t go(hb::LinearArgs &a, hipStream_t stream)
 //   64 x                                   240     114     103    69.4    49.9   [32.9]   35.7    47.2
 //   16 x (4096 -> 16384)                   239     112     104    71.4    49.9   [34.0]   35.3    46.8
 //   64 x                                   967     452     413     280     197     121     104   [97.3]
-//   64 x, groups of 32                    1160     860     555     401     222     264    [217]
+//   64 x, groups of 32                    1150     528     558     406     233     192     217    [169]
 //    8 x (512 -> 512)                     [3.6]    4.2     4.0     4.2     5.0     5.6     7.8    10.5
-// One row of many outputs (16384: 11.4 instead of 17.9) shares its digits among four tiles; up to 1024 inputs, four steps, it needs no sixteen
-// wavefronts (512 -> 1000 4.0 instead of 4.5).  Eight rows by sixteen tiles are for groups of 128: scaling every 64 or 32 inputs takes the registers of a
-// second tile.
+// One row of many outputs (16384: 11.4 instead of 17.9) shares its digits among four tiles, but for groups of 32, whose scales take the registers of four steps
+// (with two rows and two steps 16 instead of 22); up to 1024 inputs, four steps, it needs no sixteen wavefronts (512 -> 1000 4.0 instead of 4.5).
 struct Form {
     uint64_t rows, tiles, first, round;
 };
 constexpr Form kForms[] = {{1, 1, 23, 37}, {2, 1, 44, 31}, {2, 2, 24, 60}, {2, 4, 20, 83}, {4, 4, 13, 121}, {4, 8, 60, 143}, {8, 8, 125, 230},
-                           {1, 4, 44, 70}, {8, 16, 10, 480}};
+                           {8, 16, 10, 480}, {1, 4, 44, 70}};
 
 template <int FLUSH>
 hipError_t by_shape(hb::LinearArgs &a, hipStream_t stream)
@@ -46,11 +45,13 @@ hipError_t by_shape(hb::LinearArgs &a, hipStream_t stream)
     const uint64_t tiles = ((uint64_t)a.outs + 15) / 16;
     int best = 0;
     uint64_t least = ~0ull;
-    for (int i = 0; i < (int)(sizeof(kForms) / sizeof(kForms[0])); ++i) {
+    for (int i = 0; i < (FLUSH == 32 ? 8 : 9); ++i) {
         const Form &f = kForms[i];
-        if (f.tiles == 16 && FLUSH != 128) continue;
         const uint64_t blocks = (a.rows + f.rows - 1) / f.rows * ((tiles + f.tiles - 1) / f.tiles), cost = f.first + (blocks + 255) / 256 * f.round;
         if (cost < least) least = cost, best = i;
+    }
+    if constexpr (FLUSH != 32) {
+        if (best == 8) return go<1, 1, 4, 4, 4, FLUSH>(a, stream);
     }
     switch (best) {
     case 0: return a.in <= 4 * hb::kLinearStep ? go<1, 1, 1, 4, 1, FLUSH>(a, stream) : go<1, 1, 1, 16, 1, FLUSH>(a, stream);
@@ -60,10 +61,7 @@ hipError_t by_shape(hb::LinearArgs &a, hipStream_t stream)
     case 4: return go<4, 1, 4, FLUSH == 32 ? 2 : 4, 1, FLUSH>(a, stream);      // (scaling every 32 inputs takes more registers than sixteen wavefronts leave)
     case 5: return go<4, 1, 8, 1, 2, FLUSH>(a, stream);
     case 6: return go<8, 1, 8, 1, 1, FLUSH>(a, stream);
-    case 8:
-        if constexpr (FLUSH == 128) return go<8, 2, 8, 1, 1, FLUSH>(a, stream);
-        [[fallthrough]];
-    default: return go<1, 1, FLUSH == 32 ? 1 : 4, FLUSH == 32 ? 16 : 4, FLUSH == 32 ? 1 : 4, FLUSH>(a, stream);
+    default: return go<8, 2, 8, 1, 1, FLUSH>(a, stream);
     }
 }
 

@@ -63,7 +63,7 @@ __device__ __forceinline__ void store_digits(uint8_t *planes, uint32_t lane, con
 
 // A step's weights of a tile, 16 rows of 128 bytes: lane l loads 16 bytes l mod 8 of rows l / 8 and l / 8 + 8, and they go through LDS to where the matrix
 // instruction takes them.  (Loaded from there at once, 16 rows by 64 bytes an instruction, 16 cache lines are asked for in each quarter of it:
-// 64 x (4096 -> 16384) 97 us for 109, 1 x (4096 -> 4096) 5.0 for 5.5, 64 x (4096 -> 16384) in groups of 32 217 for 339.)
+// 64 x (4096 -> 16384) 97 us for 109, 1 x (4096 -> 4096) 5.0 for 5.5, 64 x (4096 -> 16384) in groups of 32 169 for 339.)
 struct StepWeights {
     u32x4_t w[2];
 };
@@ -124,7 +124,7 @@ __device__ __forceinline__ void unpack_weights(uint32_t w, int &even, int &odd)
 // A workgroup goes through the inputs in blocks of WK * P steps, whose digits its wavefronts make together and all of them read (with
 // WN = P = 1 each makes its own); wavefront (wn, wk) multiplies steps wk, wk + WK, .. of a block with its own RT tiles.
 template <int TM, int RT, int WN, int WK, int P, int FLUSH>
-__global__ void __launch_bounds__(64 * WN * WK, (TM * RT <= 8 && WK == 1 && FLUSH != 32 ? 4 : 2))
+__global__ void __launch_bounds__(64 * WN * WK, (TM * RT <= (FLUSH == 32 ? 4 : 8) && WN * WK == 8 ? 4 : 2))
 linear_q4_kernel(LinearArgs a)
 {
     constexpr int kWaves = WN * WK, kSteps = WK * P, kOwn = kSteps * TM / kWaves;      // kOwn: pieces of digits that a wavefront makes
@@ -198,7 +198,7 @@ linear_q4_kernel(LinearArgs a)
     for (uint32_t first = 0; first < steps; first += kSteps) {
         uint8_t *block = lds + buffer * kBlockBytes;
         uint32_t l = lane;
-        if constexpr (kWaves == 16) settle(l);                // (what follows from it would be kept in registers, of which sixteen wavefronts have 128)
+        if constexpr (kWaves == 16 || (FLUSH == 32 && TM * RT <= 4)) settle(l);      // (what follows from it would be kept in registers: 128 are all)
 #pragma unroll
         for (int i = 0; i < kOwn; ++i) {
             const uint32_t piece = wave * kOwn + i;

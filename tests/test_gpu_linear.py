@@ -47,7 +47,8 @@ def test_layers(inputs, outputs, group):
     _check(rng, 6, inputs, min(outputs, 520), group, 20)
 
 
-@pytest.mark.parametrize("rows,inputs,outputs,group", [(257, 130, 1100, 128), (300, 517, 1011, 256), (261, 33, 1025, 128)])
+@pytest.mark.parametrize("rows,inputs,outputs,group", [(257, 130, 1100, 128), (300, 517, 1011, 256), (261, 33, 1025, 128), (257, 130, 1100, 32),
+                                                      (259, 310, 1031, 64), (1, 700, 16500, 32), (1, 1301, 16390, 64)])
 def test_many_rows_and_outputs(rows, inputs, outputs, group):
     _check(np.random.default_rng(rows + outputs), rows, inputs, outputs, group)
 
