@@ -363,6 +363,8 @@ __device__ __forceinline__ HeadChunk head_chunk(const AttentionArgs &a, uint32_t
 
 // Scores.  A wavefront takes 16 positions at a time: a row of its tile is a key, lane l has row l mod 16 and of every 64 dimensions the pairs
 // 8 j + 2 (l / 16), j = 0 .. 7 (the lanes of a row read 64 bytes side by side).
+// What bounds it: vector-ALU issue, and the matrix instructions, which overlap little with it: of a key's number 34 instructions are its two dealer words, and a
+// score takes five more.  32768 positions of 8 heads of 128, four query heads each, 268 MB: 81 us; 81 also with all loads from one row.
 template <int GT, int ND>
 __global__ void __launch_bounds__(kAttentionBlock, 4)
 attention_scores_kernel(AttentionArgs a)
@@ -469,6 +471,7 @@ attention_scores_kernel(AttentionArgs a)
 
 // The product with the values.  A wavefront has 16 dimensions, the rows of its tile, and lane l takes 16 of every 64 positions; the workgroup, up to 128 dimensions,
 // makes the weights' vectors of CHUNK positions at a time.
+// What bounds it: as above, without the five words and the turned bytes (WHOLE); the same 32768 positions 81 us, 74 with all loads from one row.
 template <int GT, int CHUNK>
 __global__ void __launch_bounds__(kAttentionBlock, 4)
 attention_values_kernel(AttentionArgs a)
@@ -589,8 +592,7 @@ attention_values_kernel(AttentionArgs a)
     }
 }
 
-// Joins a sequence's pieces and divides by the length.  32 numbers a workgroup, whose
-// pieces eight threads each share out.
+// Joins a sequence's pieces and divides by the length.  32 numbers a workgroup, whose pieces eight threads each share out: a launch and one chain of loads, 4 to 5 us.
 constexpr int kJoinNumbers = 32, kJoinShares = kJoinBlock / kJoinNumbers;
 
 __global__ void __launch_bounds__(kJoinBlock)

@@ -123,6 +123,10 @@ __device__ __forceinline__ void unpack_weights(uint32_t w, int &even, int &odd)
 //
 // A workgroup goes through the inputs in blocks of WK * P steps, whose digits its wavefronts make together and all of them read (with
 // WN = P = 1 each makes its own); wavefront (wn, wk) multiplies steps wk, wk + WK, .. of a block with its own RT tiles.
+//
+// What bounds it: one row, the launch and the chain of loads, digits, product, join and truncation (4096 -> 4096, 9 MB, 5.0 us); many rows, the scaling (five
+// instructions for two matrix instructions) and the digits, on the vector ALU, and the matrix instructions, which overlap little with them
+// (64 rows, 4096 -> 16384, 137 T operations, 93 us: VALU 37 % of the cycles, matrix cores 27 %).
 template <int TM, int RT, int WN, int WK, int P, int FLUSH>
 __global__ void __launch_bounds__(64 * WN * WK, (TM * RT <= (FLUSH == 32 ? 4 : 8) && WN * WK == 8 ? 4 : 2))
 linear_q4_kernel(LinearArgs a)
