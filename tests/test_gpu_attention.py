@@ -103,6 +103,31 @@ def test_sequences_of_any_lengths(heads, group, dim, page, max_len, lens):
     assert bool((room[:256] == 0xA5).all()) and bool((room[256 + need:] == 0xA5).all())
 
 
+@pytest.mark.parametrize("heads,group,dim", [(2, 1, 34), (1, 4, 66), (3, 8, 16)])
+def test_replayed_with_other_lengths(heads, group, dim):
+    """One captured call on lengths that change in place: the pieces follow them."""
+    lens = [[700, 1, 0], [0, 0, 0], [3, 640, 65], [700, 700, 700], [0, 0, 129]]
+    case = Case(np.random.default_rng(dim), 3, heads, group, dim, 9, 700, lens[0])
+    cache, q0, q1, table, at, max_len, k, m, seed = case.on_gpu()
+    outs = [torch.zeros_like(q0) for _ in range(2)]
+    room = torch.empty(hb.hb_attention_workspace_bytes(cache, 3, heads * group, 700), dtype=torch.uint8, device=du.DEV)
+    graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.stream(stream), torch.cuda.graph(graph, stream=stream):
+        hb.hb_attention(cache, q0, q1, table, at, max_len, k, m, seed, outs[0], outs[1], room)
+    for now in lens + lens[::-1]:
+        case.lens = np.array(now, dtype=np.int32)
+        at.copy_(torch.from_numpy(case.lens))
+        for t in outs:
+            t.fill_(7)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, want in zip(outs, case.want()):
+            assert np.array_equal(du.host(got), want), now
+        eager = hb.hb_attention(cache, q0, q1, table, at, max_len, k, m, seed)
+        assert all(torch.equal(a, b) for a, b in zip(outs, eager[:2]))
+
+
 @pytest.mark.parametrize("group,dim", [(1, 64), (3, 18), (4, 128), (8, 40)])
 def test_any_number_of_the_ring(group, dim):
     """Keys, values and queries over all 64 bits: every carry between digits."""
