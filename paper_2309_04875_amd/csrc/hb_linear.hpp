@@ -216,6 +216,7 @@ linear_q4_kernel(LinearArgs a)
         for (int p = 0; p < P; ++p) {
             const uint32_t step = first + p * WK + wk;
             if (step >= steps) break;
+            if (p > 0) wave_exchange();                       // the weights before have been read
             int32_t now[RT][kScaleLoads];
 #pragma unroll
             for (int t = 0; t < RT; ++t) {
