@@ -2,6 +2,7 @@
 #pragma once
 
 #include "hb_digits.hpp"
+#include "hb_linear_plan.hpp"
 
 namespace hb {
 
@@ -13,11 +14,10 @@ struct LinearArgs {
     uint64_t seedA, weight_bytes;
     uint64_t group_inverse;     // ceil(2^40 / group): input / group is (input * group_inverse) >> 40
     uint32_t rows, in, outs, groups;
-    uint32_t row_tiles;
+    uint32_t row_tiles, pairs;  // tiles of rows; workgroups, a tile of rows and a group of outputs each
     int frac;
 };
 
-constexpr uint32_t kDies = 8;
 constexpr int kLinearStep = 256;                     // inputs of a step
 constexpr int kPieceBytes = 16 * kLinearStep;        // one row's digits of a step in LDS: 16 planes of a byte an input, eight of each party
 
@@ -139,10 +139,8 @@ linear_q4_kernel(LinearArgs a)
     __shared__ __align__(256) uint8_t lds[kBuffers * kBlockBytes + kWaves * RT * 2048];
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint32_t q = lane / 16, wn = wave % WN, wk = wave / WN;
-    // Workgroups with the same weights run on the same die (they are dealt out to the eight in turn), whose cache then reads them once.
-    const uint32_t place = blockIdx.x / kDies, group0 = place / a.row_tiles * kDies + blockIdx.x % kDies;
-    const uint32_t row0 = place % a.row_tiles * TM, tile0 = group0 * (WN * RT) + wn * RT;
-    if (16 * group0 * (WN * RT) >= a.outs) return;
+    const uint32_t pair = linear_pair(blockIdx.x, a.pairs), group0 = pair / a.row_tiles;
+    const uint32_t row0 = pair % a.row_tiles * TM, tile0 = group0 * (WN * RT) + wn * RT;
     const uint32_t steps = (a.in + kLinearStep - 1) / kLinearStep;
     // A lane's rows of weights and scales; outputs behind the last are the last.
     const uint8_t *weight_row[RT];

@@ -1,0 +1,41 @@
+"""How linear layers are shared out to workgroups and dies (no GPU)."""
+import numpy as np
+import pytest
+
+from plan_util import plan
+
+DIES = 8
+
+
+@pytest.mark.parametrize("count", [1, 2, 7, 8, 9, 15, 16, 17, 63, 64, 65, 256, 1000, 1024, 4099])
+def test_every_pair_once_and_all_dies_alike(count):
+    """Workgroup b runs on die b mod 8."""
+    pairs = np.array([plan().pair(b, count) for b in range(count)])
+    assert sorted(pairs) == list(range(count))
+    loads = [len(pairs[die::DIES]) for die in range(DIES)]
+    assert max(loads) - min(loads) <= 1
+    for die in range(DIES):                                          # an eighth of the pairs, in order
+        assert np.array_equal(pairs[die::DIES], pairs[die: die + 1].repeat(loads[die]) + np.arange(loads[die]))
+
+
+@pytest.mark.parametrize("rows,outs", [(2048, 1024), (2048, 256), (2048, 128), (48, 640), (64, 16384), (16, 4096), (1, 4096), (5, 1411), (1, 1)])
+@pytest.mark.parametrize("flush", [32, 64, 128])
+def test_rounds_are_those_that_the_price_counts(rows, outs, flush):
+    """The fullest die's 32 compute units go round as often as 256 of the whole card would."""
+    form = plan().form(flush, rows, outs)
+    count = plan().row_tiles(form, rows) * plan().groups(form, outs)
+    fullest = -(-count // DIES)
+    assert -(-fullest // 32) == -(-count // 256)
+
+
+def test_many_groups_stay_on_a_die():
+    """64 x (4096 -> 16384): a group's weights are read by one die's workgroups alone."""
+    rows, outs = 64, 16384
+    form = plan().form(128, rows, outs)
+    tiles, groups = plan().row_tiles(form, rows), plan().groups(form, outs)
+    count = tiles * groups
+    group_of = np.array([plan().pair(b, count) for b in range(count)]) // tiles
+    dies = {}
+    for b, g in enumerate(group_of):
+        dies.setdefault(int(g), set()).add(b % DIES)
+    assert len(dies) == groups and all(len(d) == 1 for d in dies.values())
