@@ -8,12 +8,17 @@ template <int TM, int RT, int WN, int WK, int P, int FLUSH>
 hipError_t go(hb::LinearArgs &a, hipStream_t stream)
 {
     constexpr hb::LinearForm form{TM, WN * RT, 0, 0};
-    a.row_tiles = (uint32_t)hb::linear_row_tiles(form, a.rows);
-    const uint64_t blocks = hb::linear_groups(form, a.outs) * a.row_tiles;
-    if (blocks > 0xffffffffull / (64 * WN * WK)) return hipErrorInvalidConfiguration;     // a grid has fewer than 2^32 threads
-    a.pairs = (uint32_t)blocks;
-    hipLaunchKernelGGL((hb::linear_q4_kernel<TM, RT, WN, WK, P, FLUSH>), dim3((unsigned)blocks), dim3(64 * WN * WK), 0, stream, a);
-    return hipGetLastError();
+    constexpr uint64_t threads = 64 * WN * WK;
+    const uint64_t tiles = hb::linear_row_tiles(form, a.rows), groups = hb::linear_groups(form, a.outs), most = hb::linear_launch_tiles(groups, threads);
+    for (uint64_t first = 0; first < tiles; first += most) {
+        a.first_tile = (uint32_t)first;
+        a.row_tiles = (uint32_t)(tiles - first < most ? tiles - first : most);
+        a.pairs = (uint32_t)(groups * a.row_tiles);
+        hipLaunchKernelGGL((hb::linear_q4_kernel<TM, RT, WN, WK, P, FLUSH>), dim3(a.pairs), dim3((unsigned)threads), 0, stream, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 template <int FLUSH>

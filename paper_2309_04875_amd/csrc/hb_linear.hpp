@@ -14,7 +14,7 @@ struct LinearArgs {
     uint64_t seedA, weight_bytes;
     uint64_t group_inverse;     // ceil(2^40 / group): input / group is (input * group_inverse) >> 40
     uint32_t rows, in, outs, groups;
-    uint32_t row_tiles, pairs;  // tiles of rows; workgroups, a tile of rows and a group of outputs each
+    uint32_t first_tile, row_tiles, pairs;     // of this launch: tiles of rows; workgroups, a tile of rows and a group of outputs each
     int frac;
 };
 
@@ -140,7 +140,7 @@ linear_q4_kernel(LinearArgs a)
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint32_t q = lane / 16, wn = wave % WN, wk = wave / WN;
     const uint32_t pair = linear_pair(blockIdx.x, a.pairs), group0 = pair / a.row_tiles;
-    const uint32_t row0 = pair % a.row_tiles * TM, tile0 = group0 * (WN * RT) + wn * RT;
+    const uint32_t row0 = (a.first_tile + pair % a.row_tiles) * TM, tile0 = group0 * (WN * RT) + wn * RT;
     const uint32_t steps = (a.in + kLinearStep - 1) / kLinearStep;
     // A lane's rows of weights and scales; outputs behind the last are the last.
     const uint8_t *weight_row[RT];

@@ -59,4 +59,7 @@ constexpr uint32_t linear_pair(uint32_t block, uint32_t count)
     return die * (count / kDies) + (die < more ? die : more) + block / kDies;
 }
 
+// Tiles of rows that one launch takes, three at least: a grid has fewer than 2^32 threads, and what is more goes into further launches.
+constexpr uint64_t linear_launch_tiles(uint64_t groups, uint64_t threads) { return 0xffffffffull / threads / groups; }
+
 }  // namespace hb

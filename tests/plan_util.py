@@ -17,6 +17,7 @@ extern "C" {
 int form(int flush, uint64_t rows, uint64_t outs) { return linear_form(flush, rows, outs); }
 uint64_t row_tiles(int form, uint64_t rows) { return linear_row_tiles(kLinearForm[form], rows); }
 uint64_t groups(int form, uint64_t outs) { return linear_groups(kLinearForm[form], outs); }
+uint64_t launch_tiles(uint64_t groups, uint64_t threads) { return linear_launch_tiles(groups, threads); }
 uint32_t pair(uint32_t block, uint32_t count) { return linear_pair(block, count); }
 }
 """
@@ -33,6 +34,6 @@ def plan():
         subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I" + build.CSRC, source, "-o", library], check=True)
         lib = ctypes.CDLL(library)
     u32, u64, i = ctypes.c_uint32, ctypes.c_uint64, ctypes.c_int
-    for name, result, *args in (("form", i, i, u64, u64), ("row_tiles", u64, i, u64), ("groups", u64, i, u64), ("pair", u32, u32, u32)):
+    for name, result, *args in (("form", i, i, u64, u64), ("row_tiles", u64, i, u64), ("groups", u64, i, u64), ("launch_tiles", u64, u64, u64), ("pair", u32, u32, u32)):
         getattr(lib, name).restype, getattr(lib, name).argtypes = result, args
     return lib

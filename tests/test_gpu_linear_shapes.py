@@ -24,3 +24,9 @@ def check(rng, rows, inputs, outputs, group, frac=18):
 def test_many_rows_of_few_outputs(rows, inputs, outputs, group):
     """Fewer groups of outputs than dies, or a remainder of them."""
     check(np.random.default_rng(rows), rows, inputs, outputs, group)
+
+
+@pytest.mark.parametrize("rows,inputs,outputs,group", [(1 << 24, 1, 1, 32), ((1 << 21) + 3, 2, 17, 64)])
+def test_as_many_rows_as_there_may_be(rows, inputs, outputs, group):
+    """More workgroups than one grid holds; and a size that was refused when a layer's groups were rounded up to the number of dies."""
+    check(np.random.default_rng(9), rows, inputs, outputs, group)

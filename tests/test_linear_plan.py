@@ -39,3 +39,15 @@ def test_many_groups_stay_on_a_die():
     for b, g in enumerate(group_of):
         dies.setdefault(int(g), set()).add(b % DIES)
     assert len(dies) == groups and all(len(d) == 1 for d in dies.values())
+
+
+@pytest.mark.parametrize("rows,outs", [(1 << 24, 1), (1 << 24, 16), (1 << 24, 1 << 24), (1, 1 << 24), (1 << 23, 128), ((1 << 21) - 1, 16), (1 << 22, 1000)])
+@pytest.mark.parametrize("flush", [32, 64, 128])
+def test_grids_of_the_largest_sizes(rows, outs, flush):
+    """Every size up to the stated limits has launches, each of fewer than 2^32 threads."""
+    form = plan().form(flush, rows, outs)
+    tiles, groups = plan().row_tiles(form, rows), plan().groups(form, outs)
+    assert tiles < 1 << 32
+    for threads in (256, 512, 1024):
+        most = plan().launch_tiles(groups, threads)
+        assert most >= 3 and most * groups * threads < 1 << 32 <= (most + 1) * groups * threads
