@@ -35,18 +35,6 @@ hb::CacheView view_of(const hb_cache *cache)
     return c;
 }
 
-// How the groups of numbers of all tokens go into workgroups; false: more than a grid holds.
-bool append_shape(size_t tokens, uint64_t groups, hb::AppendShape &shape)
-{
-    const uint64_t per = hb::kAppendBlock;
-    if (groups == 0) return true;
-    const uint64_t each = groups >= per ? (groups + per - 1) / per : 0, together = groups < per ? per / groups : 0;
-    const uint64_t blocks = each != 0 ? tokens * each : (tokens + together - 1) / together;
-    if (blocks > 0x7fffffffull) return false;
-    shape = hb::AppendShape{(uint32_t)blocks, (uint32_t)groups, (uint32_t)each, (uint32_t)together};
-    return true;
-}
-
 size_t round_up(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Workspace of hb_attention: shares of the scores, then the pieces' partial sums.
@@ -220,16 +208,18 @@ int hb_cache_append(const hb_cache *cache, const int64_t *k0, const int64_t *k1,
         // with 2; 333 of 36 heads of 80 9.5 and 8.8).
         const uint64_t numbers = (uint64_t)tokens * (2 * (uint64_t)cache->heads + q_heads) * cache->dim;
         const int n = rot % 4 == 0 && cache->dim % 4 == 0 && numbers >= 4ull * 256 * hb::kAppendBlock ? 2 : 1, groups = cache->dim / (2 * n);      // of a head
-        hb::AppendShape stored = {}, asked = {};
-        if (!append_shape(tokens, (uint64_t)cache->heads * groups, stored) || !append_shape(tokens, (uint64_t)q_heads * groups, asked)) return HB_EINVAL;
-        const uint64_t blocks = 2 * (uint64_t)stored.blocks + asked.blocks;
-        if (blocks > 0xffffffffull / hb::kAppendBlock) return HB_EINVAL;           // a grid has fewer than 2^32 threads
+        const uint64_t of_each = (uint64_t)cache->heads * groups, of_queries = (uint64_t)q_heads * groups, most = hb::append_launch_tokens(of_each, of_queries);
         const uint32_t head_inverse = groups == 1 ? 0 : (uint32_t)(((1ull << 32) + groups - 1) / groups);
-        const dim3 grid((unsigned)blocks), block(hb::kAppendBlock);
-        if (n == 2) hipLaunchKernelGGL(hb::cache_append_kernel<2>, grid, block, 0, (hipStream_t)stream, a, stored, asked, head_inverse);
-        else hipLaunchKernelGGL(hb::cache_append_kernel<1>, grid, block, 0, (hipStream_t)stream, a, stored, asked, head_inverse);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return hb::fail_hip(e, "kernel launch");
+        for (uint64_t first = 0; first < tokens; first += most) {
+            a.first = (uint32_t)first;
+            a.upto = (uint32_t)std::min<uint64_t>(tokens, first + most);
+            const hb::AppendShape stored = hb::append_shape(a.upto - a.first, of_each), asked = hb::append_shape(a.upto - a.first, of_queries);
+            const dim3 grid(2 * stored.blocks + asked.blocks), block(hb::kAppendBlock);
+            if (n == 2) hipLaunchKernelGGL(hb::cache_append_kernel<2>, grid, block, 0, (hipStream_t)stream, a, stored, asked, head_inverse);
+            else hipLaunchKernelGGL(hb::cache_append_kernel<1>, grid, block, 0, (hipStream_t)stream, a, stored, asked, head_inverse);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return hb::fail_hip(e, "kernel launch");
+        }
     }
     if (opened_bits) *opened_bits = 64ull * tokens * ((uint64_t)cache->heads * (rot + 2 * cache->dim) + (uint64_t)q_heads * cache->dim);
     return HB_OK;

@@ -1,6 +1,7 @@
 // Keys and values of secret-shared tokens in a paged cache of masked numbers, with the position rotation on the way.
 #pragma once
 
+#include "hb_append_plan.hpp"
 #include "hb_fixed.hpp"
 #include "hb_kernels.hpp"
 
@@ -27,24 +28,10 @@ struct AppendArgs {
     const int64_t *slots;
     const int32_t *positions, *cos, *sin; // cos, sin: [table_rows][rot / 2]
     uint64_t tokens, table_rows, seedA;
+    uint32_t first, upto;                 // tokens of this launch: first .. upto - 1
     uint32_t q_heads, rot;
     int frac;
     int32_t q_mul;
-};
-
-constexpr int kAppendBlock = 256;
-
-// What bounds it: HBM (24 bytes a key or value, 32 a query), and beside it vector-ALU issue: a rotated number takes four dealer words for its
-// truncation, and every number of the cache two for its mask, 18 instructions each.  A thread takes N neighbours (dimensions d ..) and the N that
-// turn with them (d + rot/2 ..; the next N elsewhere), so that both multiply the same row of the tables and a number's words are drawn in step;
-// N = 2 (16-byte accesses, half the addresses) where the rotated part and the rest divide into such groups: 2048 tokens of 8 + 8 + 32 heads of 128,
-// 370 MB, in 76 us (4.9 TB/s) instead of 80.  Keys, values and queries have workgroups of their own, whose wavefronts then do the same.  The groups
-// of a token are shared out to workgroups, or several tokens with few share one.
-struct AppendShape {
-    uint32_t blocks;            // of this kind (keys, values or queries)
-    uint32_t groups;            // of 2 N numbers of a token
-    uint32_t per_token;         // workgroups of a token, or 0:
-    uint32_t together;          // tokens of a workgroup
 };
 
 // N neighbouring numbers of both parties.
@@ -94,6 +81,12 @@ __device__ __forceinline__ void open_numbers(const Pair (&y)[N], uint64_t z, uin
     store_numbers<N>(to, opened);
 }
 
+// What bounds it: HBM (24 bytes a key or value, 32 a query), and beside it vector-ALU issue: a rotated number takes four dealer words for its
+// truncation, and every number of the cache two for its mask, 18 instructions each.  A thread takes N neighbours (dimensions d ..) and the N that
+// turn with them (d + rot/2 ..; the next N elsewhere), so that both multiply the same row of the tables and a number's words are drawn in step;
+// N = 2 (16-byte accesses, half the addresses) where the rotated part and the rest divide into such groups: 2048 tokens of 8 + 8 + 32 heads of 128,
+// 370 MB, in 76 us (4.9 TB/s) instead of 80.  Keys, values and queries have workgroups of their own, whose wavefronts then do the same.  The groups
+// of a token are shared out to workgroups, or several tokens with few share one.
 template <int N>
 __global__ void __launch_bounds__(kAppendBlock)
 cache_append_kernel(AppendArgs a, AppendShape stored, AppendShape asked, uint32_t head_inverse)
@@ -108,16 +101,16 @@ cache_append_kernel(AppendArgs a, AppendShape stored, AppendShape asked, uint32_
     uint64_t token;
     uint32_t item;
     if (shape.per_token != 0) {
-        token = block / shape.per_token;
+        token = a.first + block / shape.per_token;
         item = block % shape.per_token * kAppendBlock + threadIdx.x;
         if (item >= shape.groups) return;
     } else {
         const uint32_t own = threadIdx.x / shape.groups;
         if (own >= shape.together) return;
-        token = (uint64_t)block * shape.together + own;
+        token = a.first + (uint64_t)block * shape.together + own;
         item = threadIdx.x % shape.groups;
     }
-    if (token >= a.tokens) return;
+    if (token >= a.upto) return;
     const uint32_t head = groups == 1 ? item : __umulhi(item, head_inverse), group = item - head * groups;    // head_inverse: ceil(2^32 / groups)
     const bool turned = kind != 1 && N * group < half;
     const uint32_t d = kind == 1 ? 2 * N * group : turned ? N * group : a.rot + 2 * (N * group - half), apart = turned ? half : N;

@@ -1,4 +1,4 @@
-"""The launches' arithmetic (csrc/hb_linear_plan.hpp) for tests, compiled for the host."""
+"""The launches' arithmetic (csrc/hb_linear_plan.hpp, csrc/hb_append_plan.hpp) for tests, compiled for the host."""
 import ctypes
 import functools
 import os
@@ -11,6 +11,7 @@ import pytest
 from paper_2309_04875_amd import build
 
 SOURCE = r"""
+#include "hb_append_plan.hpp"
 #include "hb_linear_plan.hpp"
 using namespace hb;
 extern "C" {
@@ -19,6 +20,8 @@ uint64_t row_tiles(int form, uint64_t rows) { return linear_row_tiles(kLinearFor
 uint64_t groups(int form, uint64_t outs) { return linear_groups(kLinearForm[form], outs); }
 uint64_t launch_tiles(uint64_t groups, uint64_t threads) { return linear_launch_tiles(groups, threads); }
 uint32_t pair(uint32_t block, uint32_t count) { return linear_pair(block, count); }
+uint32_t append_blocks(uint64_t tokens, uint64_t groups) { return append_shape(tokens, groups).blocks; }
+uint64_t append_tokens(uint64_t stored, uint64_t asked) { return append_launch_tokens(stored, asked); }
 }
 """
 
@@ -34,6 +37,7 @@ def plan():
         subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I" + build.CSRC, source, "-o", library], check=True)
         lib = ctypes.CDLL(library)
     u32, u64, i = ctypes.c_uint32, ctypes.c_uint64, ctypes.c_int
-    for name, result, *args in (("form", i, i, u64, u64), ("row_tiles", u64, i, u64), ("groups", u64, i, u64), ("launch_tiles", u64, u64, u64), ("pair", u32, u32, u32)):
+    for name, result, *args in (("form", i, i, u64, u64), ("row_tiles", u64, i, u64), ("groups", u64, i, u64), ("launch_tiles", u64, u64, u64), ("pair", u32, u32, u32),
+                                ("append_blocks", u32, u64, u64), ("append_tokens", u64, u64, u64)):
         getattr(lib, name).restype, getattr(lib, name).argtypes = result, args
     return lib
