@@ -344,9 +344,10 @@ HB_API int hb_cache_append(const hb_cache *cache, const int64_t *k0, const int64
  * tensor batch x q_heads x max_len of scores with seed S_2 (elements behind a sequence's end and in holes reach no output); masks of p words 2j, 2j + 1
  * of S_3; output i words 9i .. 9i + 8 of S_4 (c_0, first and second truncation).  A product's party shares, with a the fresh mask, b the cache's, eps =
  * x - a opened now and D = y - b: c_0 + sum eps (b_0 + D) + D a_0 and (sum a b - c_0) + sum eps b_1 + D a_1.
- * workspace: DEVICE, 256-byte aligned, hb_attention_workspace_bytes(cache, batch, q_heads, max_len) bytes (0 for invalid sizes; of `cache` the sizes
- * count), overlapping nothing; contents before and after mean nothing; calls that may overlap in time need one each.  batch <= 65535,
- * max_len <= HB_ATTENTION_MAX_LEN.
+ * workspace: DEVICE, 256-byte aligned, hb_attention_workspace_bytes(cache, batch, q_heads, max_len) bytes or more (0 for invalid sizes; of `cache` the
+ * sizes count; no smaller batch or max_len needs more, so that one of the greatest serves every step), overlapping nothing; contents before and
+ * after mean nothing; calls that may overlap in time need one each.  batch <= 65535, max_len <= HB_ATTENTION_MAX_LEN,
+ * batch x q_heads x max_len <= HB_MAX_ELEMENTS.
  * opened_bits receives 192 batch q_heads dim + n (128 + hb_opened_bits per element), n = batch q_heads max_len.
  */
 HB_API int hb_attention(const hb_cache *cache, const int64_t *q0, const int64_t *q1, size_t batch, int q_heads, const int32_t *page_table,

@@ -37,7 +37,8 @@ hb::CacheView view_of(const hb_cache *cache)
 
 size_t round_up(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Workspace of hb_attention: shares of the scores, then the pieces' partial sums.
+// Workspace of hb_attention: shares of the scores, then the pieces' partial sums.  Smaller batches are cut into more pieces, so that the call itself would need
+// more room for 127 sequences than for 128: what is asked for, `bytes`, is enough for every smaller batch and max_len too.
 struct AttentionLayout {
     size_t scores1, parts, bytes;
     size_t score_pieces, value_pieces;                        // grids: pieces of a head, of all sequences (together != 0) or of the longest
@@ -104,7 +105,10 @@ AttentionLayout attention_layout(const hb_cache *cache, size_t batch, int q_head
     }
     lay.scores1 = scores;
     lay.parts = 2 * scores;
-    lay.bytes = 2 * scores + (lay.single ? 0 : round_up(16 * numbers * lay.value_pieces * (together ? 1 : batch)));
+    // Pieces of all sequences at most, also of fewer and shorter ones: as many as are cut together (512 / heads), or 1024 / heads and one more a sequence, or as
+    // one sum's most places make; a unit each at least.
+    const size_t share = std::max<size_t>(units(1024, heads), 1), pieces = std::max(batch + share, batch * units(max_len, hb::kMostPlaces));
+    lay.bytes = 2 * scores + round_up(16 * numbers * std::min(pieces, batch * units(max_len, hb::kValueUnit)));
     return lay;
 }
 
