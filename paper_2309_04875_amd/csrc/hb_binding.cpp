@@ -16,7 +16,6 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/object_ptr.h>
 
-#include <cstring>
 #include <initializer_list>
 #include <vector>
 
@@ -361,34 +360,34 @@ PyObject *linear(PyObject *, PyObject *const *a, Py_ssize_t count)
     });
 }
 
-// cache(keys, values, page_seeds) -> the bytes of its struct hb_cache
-PyObject *cache(PyObject *, PyObject *const *a, Py_ssize_t count)
+// The struct of a cache, from its three tensors as they are now.
+bool take_cache(PyObject *const *a, hb_cache &c)
 {
-    return guarded([&]() -> PyObject * {
-        if (count != 3) return not_known();
-        const at::Tensor *keys = shaped(a[0], at::kLong, {-1, -1, -1, -1}), *values = tensor_of(a[1], at::kLong);
-        hb_cache c = {};
-        if (keys == nullptr || values == nullptr || values->sizes() != keys->sizes() || !take_shaped(a[2], at::kLong, {keys->size(0)}, c.page_seeds)) return not_known();
-        for (int64_t d = 1; d < 4; ++d) {
-            if (keys->size(d) > INT32_MAX) return not_known();
-        }
-        c.keys = static_cast<int64_t *>(keys->data_ptr());
-        c.values = static_cast<int64_t *>(values->data_ptr());
-        c.pages = (size_t)keys->size(0);
-        c.heads = (int)keys->size(1);
-        c.page = (int)keys->size(2);
-        c.dim = (int)keys->size(3);
-        return PyBytes_FromStringAndSize(reinterpret_cast<const char *>(&c), sizeof(c));
-    });
-}
-bool cache_of(PyObject *o, hb_cache &c)
-{
-    if (!PyBytes_CheckExact(o) || PyBytes_GET_SIZE(o) != (Py_ssize_t)sizeof(c)) return false;
-    std::memcpy(&c, PyBytes_AS_STRING(o), sizeof(c));
+    const at::Tensor *keys = shaped(a[0], at::kLong, {-1, -1, -1, -1}), *values = tensor_of(a[1], at::kLong);
+    if (keys == nullptr || values == nullptr || values->sizes() != keys->sizes() || !take_shaped(a[2], at::kLong, {keys->size(0)}, c.page_seeds)) return false;
+    for (int64_t d = 1; d < 4; ++d) {
+        if (keys->size(d) > INT32_MAX) return false;
+    }
+    c.keys = static_cast<int64_t *>(keys->data_ptr());
+    c.values = static_cast<int64_t *>(values->data_ptr());
+    c.pages = (size_t)keys->size(0);
+    c.heads = (int)keys->size(1);
+    c.page = (int)keys->size(2);
+    c.dim = (int)keys->size(3);
     return true;
 }
 
-// append(cache, k0, k1, v0, v1, slots, positions, cos, sin, frac, seed, q0, q1, q_mul, q_out0, q_out1) -> (q_out0, q_out1, opened bits);
+// cache(keys, values, page_seeds) -> True: they are a cache's
+PyObject *cache(PyObject *, PyObject *const *a, Py_ssize_t count)
+{
+    return guarded([&]() -> PyObject * {
+        hb_cache c = {};
+        if (count != 3 || !take_cache(a, c)) return not_known();
+        Py_RETURN_TRUE;
+    });
+}
+
+// append(keys, values, page_seeds, k0, k1, v0, v1, slots, positions, cos, sin, frac, seed, q0, q1, q_mul, q_out0, q_out1) -> (q_out0, q_out1, opened bits);
 // positions, cos and sin, or the queries and their outputs, may all be None
 PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t count)
 {
@@ -396,33 +395,33 @@ PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t count)
         hb_cache c = {};
         int frac = 0, q_mul = 0;
         uint64_t seed = 0, bits = 0;
-        if (count != 16 || !cache_of(a[0], c) || !int_of(a[9], frac) || !word_of(a[10], seed) || !int_of(a[13], q_mul)) return not_known();
-        const at::Tensor *slots = shaped(a[5], at::kLong, {-1});
+        if (count != 18 || !take_cache(a, c) || !int_of(a[11], frac) || !word_of(a[12], seed) || !int_of(a[15], q_mul)) return not_known();
+        const at::Tensor *slots = shaped(a[7], at::kLong, {-1});
         if (slots == nullptr) return not_known();
         const int64_t tokens = slots->size(0);
         const int64_t *kv[4] = {}, *q[2] = {}, *to = static_cast<const int64_t *>(slots->data_ptr());
         for (int i = 0; i < 4; ++i) {
-            if (!take_shaped(a[1 + i], at::kLong, {tokens, c.heads, c.dim}, kv[i])) return not_known();
+            if (!take_shaped(a[3 + i], at::kLong, {tokens, c.heads, c.dim}, kv[i])) return not_known();
         }
         const int32_t *positions = nullptr, *cos = nullptr, *sin = nullptr;
         int64_t rows = 0, half = 0, heads = 0;
-        if (a[6] != Py_None || a[7] != Py_None || a[8] != Py_None) {
-            const at::Tensor *table = shaped(a[7], at::kInt, {-1, -1});
+        if (a[8] != Py_None || a[9] != Py_None || a[10] != Py_None) {
+            const at::Tensor *table = shaped(a[9], at::kInt, {-1, -1});
             if (table == nullptr) return not_known();
             rows = table->size(0);
             half = table->size(1);
             cos = static_cast<const int32_t *>(table->data_ptr());
-            if (half > c.dim || !take_shaped(a[8], at::kInt, {rows, half}, sin) || !take_shaped(a[6], at::kInt, {tokens}, positions)) return not_known();
+            if (half > c.dim || !take_shaped(a[10], at::kInt, {rows, half}, sin) || !take_shaped(a[8], at::kInt, {tokens}, positions)) return not_known();
         }
         int64_t *o[2] = {};
-        if (a[11] != Py_None || a[12] != Py_None) {
-            const at::Tensor *query = shaped(a[11], at::kLong, {tokens, -1, c.dim});
+        if (a[13] != Py_None || a[14] != Py_None) {
+            const at::Tensor *query = shaped(a[13], at::kLong, {tokens, -1, c.dim});
             if (query == nullptr || query->size(1) > INT32_MAX) return not_known();
             heads = query->size(1);
             q[0] = static_cast<const int64_t *>(query->data_ptr());
-            if (!take_shaped(a[12], at::kLong, {tokens, heads, c.dim}, q[1])) return not_known();
+            if (!take_shaped(a[14], at::kLong, {tokens, heads, c.dim}, q[1])) return not_known();
             for (int i = 0; i < 2; ++i) {
-                if (!take_shaped(a[14 + i], at::kLong, {tokens, heads, c.dim}, o[i])) return not_known();
+                if (!take_shaped(a[16 + i], at::kLong, {tokens, heads, c.dim}, o[i])) return not_known();
             }
         }
         void *stream = current_stream();
@@ -430,30 +429,30 @@ PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t count)
             return hb_cache_append(&c, kv[0], kv[1], kv[2], kv[3], (size_t)tokens, to, positions, cos, sin, (size_t)rows, (int)(2 * half), frac, q[0], q[1],
                                    (int)heads, q_mul, seed, o[0], o[1], &bits, stream);
         });
-        return checked(st, st == HB_OK ? Py_BuildValue("OOK", a[14], a[15], (unsigned long long)bits) : nullptr);
+        return checked(st, st == HB_OK ? Py_BuildValue("OOK", a[16], a[17], (unsigned long long)bits) : nullptr);
     });
 }
 
-// attention(cache, q0, q1, page_table, lens, max_len, k, m, seed, out0, out1, workspace) -> (out0, out1, opened bits)
+// attention(keys, values, page_seeds, q0, q1, page_table, lens, max_len, k, m, seed, out0, out1, workspace) -> (out0, out1, opened bits)
 PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t count)
 {
     return guarded([&]() -> PyObject * {
         hb_cache c = {};
         int max_len = 0, k = 0, m = 0;
         uint64_t seed = 0, wide = 0, bits = 0;
-        if (count != 12 || !cache_of(a[0], c) || !int_of(a[5], max_len) || !word_of(a[5], wide) || !int_of(a[6], k) || !int_of(a[7], m) || !word_of(a[8], seed) ||
+        if (count != 14 || !take_cache(a, c) || !int_of(a[7], max_len) || !word_of(a[7], wide) || !int_of(a[8], k) || !int_of(a[9], m) || !word_of(a[10], seed) ||
             wide > INT32_MAX)
             return not_known();
-        const at::Tensor *query = shaped(a[1], at::kLong, {-1, -1, c.dim}), *workspace = shaped(a[11], at::kByte, {-1});
+        const at::Tensor *query = shaped(a[3], at::kLong, {-1, -1, c.dim}), *workspace = shaped(a[13], at::kByte, {-1});
         if (query == nullptr || workspace == nullptr || query->size(1) > INT32_MAX) return not_known();
         const int64_t batch = query->size(0), heads = query->size(1);
-        const at::Tensor *table = shaped(a[3], at::kInt, {batch, -1});
+        const at::Tensor *table = shaped(a[5], at::kInt, {batch, -1});
         const int64_t *q0 = static_cast<const int64_t *>(query->data_ptr()), *q1 = nullptr;
         int64_t *o[2] = {};
         const int32_t *lens = nullptr;
-        if (table == nullptr || !take_shaped(a[2], at::kLong, {batch, heads, c.dim}, q1) || !take_shaped(a[4], at::kInt, {batch}, lens)) return not_known();
+        if (table == nullptr || !take_shaped(a[4], at::kLong, {batch, heads, c.dim}, q1) || !take_shaped(a[6], at::kInt, {batch}, lens)) return not_known();
         for (int i = 0; i < 2; ++i) {
-            if (!take_shaped(a[9 + i], at::kLong, {batch, heads, c.dim}, o[i])) return not_known();
+            if (!take_shaped(a[11 + i], at::kLong, {batch, heads, c.dim}, o[i])) return not_known();
         }
         const int32_t *pages = static_cast<const int32_t *>(table->data_ptr());
         const size_t width = (size_t)table->size(1), room = (size_t)workspace->numel();
@@ -461,7 +460,7 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t count)
         const int st = without_gil([&] {
             return hb_attention(&c, q0, q1, (size_t)batch, (int)heads, pages, width, lens, (size_t)max_len, k, m, seed, o[0], o[1], to, room, &bits, stream);
         });
-        return checked(st, st == HB_OK ? Py_BuildValue("OOK", a[9], a[10], (unsigned long long)bits) : nullptr);
+        return checked(st, st == HB_OK ? Py_BuildValue("OOK", a[11], a[12], (unsigned long long)bits) : nullptr);
     });
 }
 
@@ -484,7 +483,7 @@ PyMethodDef g_methods[] = {
     HB_FAST(eco_scan, "zero-error scan"),
     HB_FAST(party, "party-faithful ReLU"),
     HB_FAST(linear, "linear layer with 4-bit weights"),
-    HB_FAST(cache, "struct of a paged cache"),
+    HB_FAST(cache, "tensors of a paged cache"),
     HB_FAST(append, "keys and values into a paged cache"),
     HB_FAST(attention, "attention over a paged cache"),
     {"plan_run", plan_run, METH_O, "enqueue a plan"},

@@ -657,23 +657,28 @@ def hb_linear_q4(x0, x1, weight, scales, group, frac, seed, out0=None, out1=None
 
 
 class Cache:
-    """A paged cache (struct hb_cache): keys, values int64 [pages, heads, tokens per page, dim], page_seeds int64 [pages]; keeps the tensors."""
+    """A paged cache (struct hb_cache): keys, values int64 [pages, heads, tokens per page, dim], page_seeds int64 [pages].  Every call takes the three
+    tensors as they are then: a cache grows by tensors put in their place."""
 
     def __init__(self, keys, values, page_seeds):
         self.keys, self.values, self.page_seeds = keys, values, page_seeds
-        self.struct = _native.cache(keys, values, page_seeds)            # its bytes
-        if self.struct is NotImplemented:
-            import torch
-            at = _typed(keys, torch.int64, None, None, None, None), _typed(values, torch.int64, *keys.shape), _typed(page_seeds, torch.int64, keys.shape[0])
-            if max(keys.shape[1:]) >= 1 << 31:
-                raise ValueError("a cache's sizes are ints")
-            self.struct = bytes(hb_cache(*at, *keys.shape))
+        if _native.cache(keys, values, page_seeds) is NotImplemented:
+            _cache_arg(self)
+
+    @property
+    def struct(self):
+        return bytes(_cache_arg(self))
 
 
 def _cache_arg(cache):
+    import torch
     if not isinstance(cache, Cache):
         raise TypeError("expected a Cache")
-    return hb_cache.from_buffer_copy(cache.struct)
+    keys, values, page_seeds = cache.keys, cache.values, cache.page_seeds
+    at = _typed(keys, torch.int64, None, None, None, None), _typed(values, torch.int64, *keys.shape), _typed(page_seeds, torch.int64, keys.shape[0])
+    if max(keys.shape[1:]) >= 1 << 31:
+        raise ValueError("a cache's sizes are ints")
+    return hb_cache(*at, *keys.shape)
 
 
 def hb_cache_append(cache, k0, k1, v0, v1, slots, positions, cos, sin, frac, seed, q0=None, q1=None, q_mul=0, q_out0=None, q_out1=None,
@@ -683,7 +688,7 @@ def hb_cache_append(cache, k0, k1, v0, v1, slots, positions, cos, sin, frac, see
     returns (q_out0, q_out1, opened_bits), the outputs None without queries."""
     import torch
     if stream is None and type(cache) is Cache:
-        done = _native.append(cache.struct, k0, k1, v0, v1, slots, positions, cos, sin, frac, seed, q0, q1, q_mul, q_out0, q_out1)
+        done = _native.append(cache.keys, cache.values, cache.page_seeds, k0, k1, v0, v1, slots, positions, cos, sin, frac, seed, q0, q1, q_mul, q_out0, q_out1)
         if done is not NotImplemented:
             return done
     cache = _cache_arg(cache)
@@ -717,7 +722,7 @@ def hb_attention(cache, q0, q1, page_table, lens, max_len, k, m, seed, out0=None
     unless one is passed."""
     import torch
     if stream is None and type(cache) is Cache:
-        done = _native.attention(cache.struct, q0, q1, page_table, lens, max_len, k, m, seed, out0, out1, workspace)
+        done = _native.attention(cache.keys, cache.values, cache.page_seeds, q0, q1, page_table, lens, max_len, k, m, seed, out0, out1, workspace)
         if done is not NotImplemented:
             return done
     pointer = ctypes.byref(_cache_arg(cache))
