@@ -66,6 +66,16 @@ bool int_of(PyObject *o, int &v)
     return known;
 }
 
+// An int that is one: others are the Python function's to refuse.
+bool plain_int_of(PyObject *o, int &v)
+{
+    if (!PyLong_CheckExact(o)) return false;
+    int over = 0;
+    const long w = PyLong_AsLongAndOverflow(o, &over);
+    v = (int)w;
+    return over == 0 && w == v;
+}
+
 void *current_stream() { return c10::hip::getCurrentHIPStream(c10::hip::current_device()).stream(); }
 
 // The result of a call, or the exception of its status.
@@ -335,7 +345,7 @@ PyObject *linear(PyObject *, PyObject *const *a, Py_ssize_t count)
     return guarded([&]() -> PyObject * {
         int group = 0, frac = 0;
         uint64_t seed = 0, bits = 0;
-        if (count != 9 || !int_of(a[4], group) || !int_of(a[5], frac) || !word_of(a[6], seed) || group < 1) return not_known();
+        if (count != 9 || !plain_int_of(a[4], group) || !plain_int_of(a[5], frac) || !word_of(a[6], seed) || group < 1) return not_known();
         const at::Tensor *x = tensor_of(a[0], at::kLong), *weight = shaped(a[2], at::kByte, {-1, -1});
         if (x == nullptr || weight == nullptr || x->dim() < 1) return not_known();
         const int64_t in = x->size(-1), out = weight->size(0);
@@ -395,7 +405,7 @@ PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t count)
         hb_cache c = {};
         int frac = 0, q_mul = 0;
         uint64_t seed = 0, bits = 0;
-        if (count != 18 || !take_cache(a, c) || !int_of(a[11], frac) || !word_of(a[12], seed) || !int_of(a[15], q_mul)) return not_known();
+        if (count != 18 || !take_cache(a, c) || !plain_int_of(a[11], frac) || !word_of(a[12], seed) || !plain_int_of(a[15], q_mul)) return not_known();
         const at::Tensor *slots = shaped(a[7], at::kLong, {-1});
         if (slots == nullptr) return not_known();
         const int64_t tokens = slots->size(0);
@@ -439,9 +449,8 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t count)
     return guarded([&]() -> PyObject * {
         hb_cache c = {};
         int max_len = 0, k = 0, m = 0;
-        uint64_t seed = 0, wide = 0, bits = 0;
-        if (count != 14 || !take_cache(a, c) || !int_of(a[7], max_len) || !word_of(a[7], wide) || !int_of(a[8], k) || !int_of(a[9], m) || !word_of(a[10], seed) ||
-            wide > INT32_MAX)
+        uint64_t seed = 0, bits = 0;
+        if (count != 14 || !take_cache(a, c) || !plain_int_of(a[7], max_len) || !plain_int_of(a[8], k) || !plain_int_of(a[9], m) || !word_of(a[10], seed) || max_len < 0)
             return not_known();
         const at::Tensor *query = shaped(a[3], at::kLong, {-1, -1, c.dim}), *workspace = shaped(a[13], at::kByte, {-1});
         if (query == nullptr || workspace == nullptr || query->size(1) > INT32_MAX) return not_known();

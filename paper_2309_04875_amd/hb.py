@@ -617,6 +617,14 @@ def _typed(t, dtype, *shape):
     return t.data_ptr()
 
 
+def _number(value, name, bits=31):
+    """A whole number that is given to C as it is: ctypes takes the lower bits of larger ones."""
+    value = int(value)
+    if not -(1 << bits) <= value < 1 << bits:
+        raise ValueError("%s = %d is out of range" % (name, value))
+    return value
+
+
 def _made_for(stream, make):
     """What make() allocates, as memory of the stream that the call runs on: torch then gives none of it to another stream's tensors, or
     theirs to it, before the work has ended."""
@@ -639,7 +647,7 @@ def hb_linear_q4(x0, x1, weight, scales, group, frac, seed, out0=None, out1=None
             return done
     if not isinstance(x0, torch.Tensor) or not isinstance(weight, torch.Tensor):
         raise TypeError("expected CUDA tensors")
-    group = int(group)
+    group, frac = _number(group, "group"), _number(frac, "frac")
     inputs, outputs = x0.shape[-1] if x0.dim() else 0, weight.shape[0] if weight.dim() else 0
     if inputs < 1 or group < 1:
         raise ValueError("a linear layer has inputs, and groups of them")
@@ -651,7 +659,7 @@ def hb_linear_q4(x0, x1, weight, scales, group, frac, seed, out0=None, out1=None
     at = [_typed(x0, torch.int64, *lead, inputs), _typed(x1, torch.int64, *lead, inputs), _typed(weight, torch.uint8, outputs, (inputs + 1) // 2),
           _typed(scales, torch.int32, outputs, -(-inputs // group)), _typed(out0, torch.int64, *lead, outputs), _typed(out1, torch.int64, *lead, outputs)]
     bits = ctypes.c_uint64(0)
-    _check(load().hb_linear_q4(at[0], at[1], x0.numel() // inputs, inputs, outputs, at[2], at[3], group, int(frac), int(seed) & (2**64 - 1), at[4],
+    _check(load().hb_linear_q4(at[0], at[1], x0.numel() // inputs, inputs, outputs, at[2], at[3], group, frac, int(seed) & (2**64 - 1), at[4],
                                at[5], ctypes.byref(bits), _stream_handle(stream)))
     return out0, out1, int(bits.value)
 
@@ -684,14 +692,14 @@ def _cache_arg(cache):
 def hb_cache_append(cache, k0, k1, v0, v1, slots, positions, cos, sin, frac, seed, q0=None, q1=None, q_mul=0, q_out0=None, q_out1=None,
                     stream=None):
     """Append keys and values [tokens, heads, dim] at slots (int64 [tokens], out of range: padding), keys and queries [tokens, q_heads, dim] rotated
-    by rows positions (int32 [tokens]) of cos and sin (int32 [rows, rot / 2] at 2^frac; all three None: no rotation), queries times q_mul / 2^frac;
-    returns (q_out0, q_out1, opened_bits), the outputs None without queries."""
+    by rows positions (int32 [tokens]) of cos and sin (int32 [rows, rot / 2] at 2^frac; all three None: no rotation), queries times q_mul / 2^frac
+    (q_mul: int32); returns (q_out0, q_out1, opened_bits), the outputs None without queries."""
     import torch
     if stream is None and type(cache) is Cache:
         done = _native.append(cache.keys, cache.values, cache.page_seeds, k0, k1, v0, v1, slots, positions, cos, sin, frac, seed, q0, q1, q_mul, q_out0, q_out1)
         if done is not NotImplemented:
             return done
-    cache = _cache_arg(cache)
+    cache, frac, q_mul = _cache_arg(cache), _number(frac, "frac"), _number(q_mul, "q_mul")
     tokens = slots.shape[0] if isinstance(slots, torch.Tensor) and slots.dim() else 0
     kv = [_typed(t, torch.int64, tokens, cache.heads, cache.dim) for t in (k0, k1, v0, v1)]
     rows, half, turn = 0, 0, [None, None, None]
@@ -707,13 +715,14 @@ def hb_cache_append(cache, k0, k1, v0, v1, slots, positions, cos, sin, frac, see
             q_out1 = _made_for(stream, lambda: torch.empty_like(q1))
         q = [_typed(t, torch.int64, tokens, heads, cache.dim) for t in (q0, q1, q_out0, q_out1)]
     bits = ctypes.c_uint64(0)
-    _check(load().hb_cache_append(ctypes.byref(cache), *kv, tokens, _typed(slots, torch.int64, tokens), *turn, rows, 2 * half, int(frac), q[0], q[1], heads,
-                                  int(q_mul), int(seed) & (2**64 - 1), q[2], q[3], ctypes.byref(bits), _stream_handle(stream)))
+    _check(load().hb_cache_append(ctypes.byref(cache), *kv, tokens, _typed(slots, torch.int64, tokens), *turn, rows, _number(2 * half, "rot"), frac, q[0], q[1],
+                                  _number(heads, "q_heads"), q_mul, int(seed) & (2**64 - 1), q[2], q[3], ctypes.byref(bits), _stream_handle(stream)))
     return q_out0, q_out1, int(bits.value)
 
 
 def hb_attention_workspace_bytes(cache, batch, q_heads, max_len):
-    return int(load().hb_attention_workspace_bytes(ctypes.byref(_cache_arg(cache)), int(batch), int(q_heads), int(max_len)))
+    return int(load().hb_attention_workspace_bytes(ctypes.byref(_cache_arg(cache)), _number(batch, "batch", 63), _number(q_heads, "q_heads"),
+                                                   _number(max_len, "max_len", 63)))
 
 
 def hb_attention(cache, q0, q1, page_table, lens, max_len, k, m, seed, out0=None, out1=None, workspace=None, stream=None):
@@ -726,6 +735,7 @@ def hb_attention(cache, q0, q1, page_table, lens, max_len, k, m, seed, out0=None
         if done is not NotImplemented:
             return done
     pointer = ctypes.byref(_cache_arg(cache))
+    k, m, max_len = _number(k, "k"), _number(m, "m"), _number(max_len, "max_len", 63)
     if out0 is None:
         out0 = _made_for(stream, lambda: torch.empty_like(q0))
     if out1 is None:
@@ -735,11 +745,11 @@ def hb_attention(cache, q0, q1, page_table, lens, max_len, k, m, seed, out0=None
     at += [_typed(t, torch.int64, batch, heads, dim) for t in (q1, out0, out1)]
     at += [_typed(page_table, torch.int32, batch, None), _typed(lens, torch.int32, batch)]
     if workspace is None:
-        need = int(load().hb_attention_workspace_bytes(pointer, batch, heads, int(max_len)))
+        need = int(load().hb_attention_workspace_bytes(pointer, batch, _number(heads, "q_heads"), max_len))
         workspace = _made_for(stream, lambda: torch.empty(max(need, 256), dtype=torch.uint8, device=q0.device))
     room = _typed(workspace, torch.uint8, None)
     bits = ctypes.c_uint64(0)
-    _check(load().hb_attention(pointer, at[0], at[1], batch, heads, at[4], page_table.shape[1], at[5], int(max_len), int(k), int(m),
+    _check(load().hb_attention(pointer, at[0], at[1], batch, _number(heads, "q_heads"), at[4], page_table.shape[1], at[5], max_len, k, m,
                                int(seed) & (2**64 - 1), at[2], at[3], room, workspace.numel(), ctypes.byref(bits), _stream_handle(stream)))
     return out0, out1, int(bits.value)
 
