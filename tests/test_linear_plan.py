@@ -2,6 +2,7 @@
 import numpy as np
 import pytest
 
+import linear_cases
 from plan_util import plan
 
 DIES = 8
@@ -51,3 +52,13 @@ def test_grids_of_the_largest_sizes(rows, outs, flush):
     for threads in (256, 512, 1024):
         most = plan().launch_tiles(groups, threads)
         assert most >= 3 and most * groups * threads < 1 << 32 <= (most + 1) * groups * threads
+
+
+@pytest.mark.parametrize("form,rows,inputs,outs,group", linear_cases.cases())
+def test_the_gpu_tests_reach_the_forms_that_they_say(form, rows, inputs, outs, group):
+    assert plan().form(group, rows, outs) == form
+
+
+def test_every_form_has_cases():
+    for group in linear_cases.GROUPS:
+        assert {case[0] for case in linear_cases.cases() if case[4] == group} == set(range(8 if group == 32 else 9))
