@@ -270,7 +270,7 @@ struct Planes {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) z[j] = state(start, 4 * s + j);
                 Flipped<8> words;
-                mix_flipped<true>(z, words);
+                mix_flipped(z, words);
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     Numbers4 four;

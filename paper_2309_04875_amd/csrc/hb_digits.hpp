@@ -35,47 +35,34 @@ struct Flipped {
 
 // Dealer words of N states, flipped: the last xor of the generator takes the flip along.  (Halves, for a register each: as 64-bit numbers they would be moved to
 // where four of a half lie side by side, an instruction and a half a word.)
-template <bool RUNS, int N>
-__device__ __forceinline__ void mix_flipped(uint64_t (&z)[N], Flipped<N> &out)
+template <int N>
+__device__ __forceinline__ void mix_flipped(uint64_t (&z)[N], Flipped<N> &out)         // (in step: as in mix_words)
 {
-    auto last = [&](uint64_t (&t)[N]) {
+    settle(z);
+    priority<true, kElsewhere>();
+    xor_shift(z, 30);
+    settle(z);
+    priority<true, kElsewhere>();
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            out.low[i] = bitop3<kTtXor3>((uint32_t)z[i], (uint32_t)t[i], kDigitFlip);
-            out.high[i] = bitop3<kTtXor3>((uint32_t)(z[i] >> 32), (uint32_t)(t[i] >> 32), kDigitFlip);
-        }
-    };
+    for (int i = 0; i < N; ++i) z[i] *= 0xBF58476D1CE4E5B9ull;
+    xor_shift(z, 27);
+    settle(z);
+    priority<true, kElsewhere>();
+#pragma unroll
+    for (int i = 0; i < N; ++i) z[i] *= 0x94D049BB133111EBull;
     uint64_t t[N];
-    if constexpr (RUNS) {                                      // as in mix_words
-        settle(z);
-        priority<true, kElsewhere>();
-        xor_shift(z, 30);
-        settle(z);
-        priority<true, kElsewhere>();
 #pragma unroll
-        for (int i = 0; i < N; ++i) z[i] *= 0xBF58476D1CE4E5B9ull;
-        xor_shift(z, 27);
-        settle(z);
-        priority<true, kElsewhere>();
+    for (int i = 0; i < N; ++i) t[i] = z[i] >> 31;
+    settle(t);
+    priority<true, kXorRuns>();
 #pragma unroll
-        for (int i = 0; i < N; ++i) z[i] *= 0x94D049BB133111EBull;
-#pragma unroll
-        for (int i = 0; i < N; ++i) t[i] = z[i] >> 31;
-        settle(t);
-        priority<true, kXorRuns>();
-        last(t);
-        settle(out.low);
-        settle(out.high);
-        priority<true, kElsewhere>();
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            z[i] = (z[i] ^ (z[i] >> 30)) * 0xBF58476D1CE4E5B9ull;
-            z[i] = (z[i] ^ (z[i] >> 27)) * 0x94D049BB133111EBull;
-            t[i] = z[i] >> 31;
-        }
-        last(t);
+    for (int i = 0; i < N; ++i) {
+        out.low[i] = bitop3<kTtXor3>((uint32_t)z[i], (uint32_t)t[i], kDigitFlip);
+        out.high[i] = bitop3<kTtXor3>((uint32_t)(z[i] >> 32), (uint32_t)(t[i] >> 32), kDigitFlip);
     }
+    settle(out.low);
+    settle(out.high);
+    priority<true, kElsewhere>();
 }
 
 // Digits of four numbers: out[i] holds digit i of v[0] .. v[3], one byte each.

@@ -134,7 +134,9 @@ linear_q4_kernel(LinearArgs a)
     constexpr int kWaves = WN * WK, kSteps = WK * P, kOwn = kSteps * TM / kWaves;      // kOwn: pieces of digits that a wavefront makes
     static_assert(kOwn * kWaves == kSteps * TM, "every wavefront makes as many pieces");
     constexpr bool kShared = WN > 1 || P > 1;
-    constexpr int kBlockBytes = kSteps * TM * kPieceBytes, kBuffers = kShared && 2 * kBlockBytes + kWaves * RT * 2048 <= 160 * 1024 ? 2 : 1;
+    // Shared digits of two blocks: one is written while the one before is still read.
+    constexpr int kBlockBytes = kSteps * TM * kPieceBytes, kBuffers = kShared ? 2 : 1;
+    static_assert(kBuffers * kBlockBytes + kWaves * RT * 2048 <= 160 * 1024, "LDS of a compute unit");
     static_assert(kWaves * RT * TM * 256 <= kBuffers * kBlockBytes, "the sums' exchange takes the digits' place");
     __shared__ __align__(256) uint8_t lds[kBuffers * kBlockBytes + kWaves * RT * 2048];
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -209,7 +211,7 @@ linear_q4_kernel(LinearArgs a)
         load_rows(first + kSteps);
         if constexpr (kShared) __syncthreads();
         else wave_exchange();
-        if constexpr (kBuffers == 2) buffer ^= 1;             // the next block's digits go to the other one
+        if constexpr (kShared) buffer ^= 1;                   // the next block's digits go to the other one
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             const uint32_t step = first + p * WK + wk;
@@ -285,7 +287,6 @@ linear_q4_kernel(LinearArgs a)
             }
         }
         if constexpr (!kShared) wave_exchange();              // the digits have been read
-        else if constexpr (kBuffers == 1) __syncthreads();
     }
     // A lane's four digits of party q / 2, upper or lower half; then the other half's and the other wavefronts'.
     __syncthreads();
