@@ -159,7 +159,7 @@ linear_q4_kernel(LinearArgs a)
     uint8_t *my_weights = lds + kBuffers * kBlockBytes + wave * (RT * 2048);
     const uint32_t last_out = 16 * (tile0 + RT) < a.outs ? 16 * (tile0 + RT) - 1 : a.outs - 1;
     const uint64_t last_row = (uint64_t)last_out * row_bytes;
-    int64_t sum[TM][RT][2] = {};
+    uint64_t sum[TM][RT][2] = {};                             // mod 2^64: a long row of large scales goes round
     // Scales: lane quarter q loads that of the q-th FLUSH inputs of every four in a step.
     constexpr int kScales = 128 / FLUSH, kScaleLoads = FLUSH == 32 ? 2 : 1;
     StepWeights weights[P][RT];
@@ -255,8 +255,8 @@ linear_q4_kernel(LinearArgs a)
                         for (int t = 0; t < RT; ++t) {
                             const i32x4_t &s = part[m % 2][t];
                             const int low = (s[0] >> 4) + s[1] * 16, high = s[2] + s[3] * 256;
-                            sum[m][t][0] += (int64_t)low * scale[t][f];
-                            sum[m][t][1] += (int64_t)high * scale[t][f];
+                            sum[m][t][0] += (uint64_t)((int64_t)low * scale[t][f]);
+                            sum[m][t][1] += (uint64_t)((int64_t)high * scale[t][f]);
                         }
                     };
 #pragma unroll
@@ -296,7 +296,7 @@ linear_q4_kernel(LinearArgs a)
     for (int m = 0; m < TM; ++m) {
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
-            uint64_t y = (uint64_t)sum[m][t][0] + ((uint64_t)(sum[m][t][1] >> 4) << 16);
+            uint64_t y = sum[m][t][0] + (sum[m][t][1] >> 4 << 16);
             if (q & 1) y <<= 32;
             y += __shfl_xor((unsigned long long)y, 16, 64);
             if ((q & 1) == 0) sums[wk * kSums + ((m * WN + wn) * RT + t) * 32 + 16 * (q / 2) + lane % 16] = y;
