@@ -189,21 +189,9 @@ int hb_cache_append(const hb_cache *cache, const int64_t *k0, const int64_t *k1,
         }
         hb::AppendArgs a = {};
         a.cache = view_of(cache);
-        const int64_t *const in[6] = {k0, k1, v0, v1, q0, q1};
-        for (int p = 0; p < 2; ++p) {
-            a.k[p] = (const uint64_t *)in[p];
-            a.v[p] = (const uint64_t *)in[2 + p];
-            a.q[p] = (const uint64_t *)in[4 + p];
-        }
-        a.qo[0] = (uint64_t *)q_out0;
-        a.qo[1] = (uint64_t *)q_out1;
-        a.slots = slots;
-        a.positions = positions;
         a.cos = cos;
         a.sin = sin;
-        a.tokens = tokens;
         a.table_rows = table_rows;
-        a.seedA = hb::stream_word(seed, 1);
         a.q_heads = (uint32_t)q_heads;
         a.rot = (uint32_t)rot;
         a.frac = frac;
@@ -215,9 +203,24 @@ int hb_cache_append(const hb_cache *cache, const int64_t *k0, const int64_t *k1,
         const uint64_t of_each = (uint64_t)cache->heads * groups, of_queries = (uint64_t)q_heads * groups, most = hb::append_launch_tokens(of_each, of_queries);
         const uint32_t head_inverse = groups == 1 ? 0 : (uint32_t)(((1ull << 32) + groups - 1) / groups);
         for (uint64_t first = 0; first < tokens; first += most) {
-            a.first = (uint32_t)first;
-            a.upto = (uint32_t)std::min<uint64_t>(tokens, first + most);
-            const hb::AppendShape stored = hb::append_shape(a.upto - a.first, of_each), asked = hb::append_shape(a.upto - a.first, of_queries);
+            const uint64_t here = std::min<uint64_t>(tokens - first, most), keys = first * cache->heads * cache->dim, queries = first * q_heads * cache->dim;
+            const int64_t *const in[4] = {k0, k1, v0, v1};
+            for (int p = 0; p < 2; ++p) {
+                a.k[p] = (const uint64_t *)in[p] + keys;
+                a.v[p] = (const uint64_t *)in[2 + p] + keys;
+            }
+            if (q_heads != 0) {
+                a.q[0] = (const uint64_t *)q0 + queries;
+                a.q[1] = (const uint64_t *)q1 + queries;
+                a.qo[0] = (uint64_t *)q_out0 + queries;
+                a.qo[1] = (uint64_t *)q_out1 + queries;
+            }
+            a.slots = slots + first;
+            a.positions = rot != 0 ? positions + first : nullptr;
+            a.tokens = here;
+            a.seedA = hb::stream_word(seed, 1) + hb::kTruncateWords * keys * hb::kGamma;          // the state `keys` numbers on
+            a.queries_at = (uint64_t)tokens * cache->heads * cache->dim + queries - keys;
+            const hb::AppendShape stored = hb::append_shape(here, of_each), asked = hb::append_shape(here, of_queries);
             const dim3 grid(2 * stored.blocks + asked.blocks), block(hb::kAppendBlock);
             if (n == 2) hipLaunchKernelGGL(hb::cache_append_kernel<2>, grid, block, 0, (hipStream_t)stream, a, stored, asked, head_inverse);
             else hipLaunchKernelGGL(hb::cache_append_kernel<1>, grid, block, 0, (hipStream_t)stream, a, stored, asked, head_inverse);

@@ -27,8 +27,8 @@ struct AppendArgs {
     uint64_t *qo[2];
     const int64_t *slots;
     const int32_t *positions, *cos, *sin; // cos, sin: [table_rows][rot / 2]
-    uint64_t tokens, table_rows, seedA;
-    uint32_t first, upto;                 // tokens of this launch: first .. upto - 1
+    uint64_t tokens, table_rows, seedA;   // of this launch, as are the addresses above but for the tables
+    uint64_t queries_at;                  // number of the first query, as dealer words count them, beyond that of the first key
     uint32_t q_heads, rot;
     int frac;
     int32_t q_mul;
@@ -101,16 +101,16 @@ cache_append_kernel(AppendArgs a, AppendShape stored, AppendShape asked, uint32_
     uint64_t token;
     uint32_t item;
     if (shape.per_token != 0) {
-        token = a.first + block / shape.per_token;
+        token = block / shape.per_token;
         item = block % shape.per_token * kAppendBlock + threadIdx.x;
         if (item >= shape.groups) return;
     } else {
         const uint32_t own = threadIdx.x / shape.groups;
         if (own >= shape.together) return;
-        token = a.first + (uint64_t)block * shape.together + own;
+        token = (uint64_t)block * shape.together + own;
         item = threadIdx.x % shape.groups;
     }
-    if (token >= a.upto) return;
+    if (token >= a.tokens) return;
     const uint32_t head = groups == 1 ? item : __umulhi(item, head_inverse), group = item - head * groups;    // head_inverse: ceil(2^32 / groups)
     const bool turned = kind != 1 && N * group < half;
     const uint32_t d = kind == 1 ? 2 * N * group : turned ? N * group : a.rot + 2 * (N * group - half), apart = turned ? half : N;
@@ -124,13 +124,18 @@ cache_append_kernel(AppendArgs a, AppendShape stored, AppendShape asked, uint32_
     if (slot < 0 || (uint64_t)slot >= (uint64_t)c.pages * c.page) return;
     if (half != 0 && (position < 0 || (uint64_t)position >= a.table_rows)) return;
     if (turned || kind == 2) {
+        int32_t cos[N] = {}, sin[N] = {};                // both are asked for before either is waited for
+        if (turned) {
+            const uint64_t from = position * half + N * group;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                cos[j] = a.cos[from + j];
+                sin[j] = a.sin[from + j];
+            }
+        }
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            int64_t co = (int64_t)1 << a.frac, si = 0;
-            if (turned) {
-                co = a.cos[position * half + N * group + j];
-                si = a.sin[position * half + N * group + j];
-            }
+            int64_t co = turned ? cos[j] : (int64_t)1 << a.frac, si = sin[j];
             if (kind == 2) {                         // the public factor goes into the table, rounded to its precision
                 const int64_t round = (int64_t)1 << (a.frac - 1);
                 co = (co * a.q_mul + round) >> a.frac;
@@ -141,7 +146,7 @@ cache_append_kernel(AppendArgs a, AppendShape stored, AppendShape asked, uint32_
             y0[j] = Pair{u.p0 * cu - w.p0 * su, u.p1 * cu - w.p1 * su};
             y1[j] = Pair{w.p0 * cu + u.p0 * su, w.p1 * cu + u.p1 * su};
         }
-        const uint64_t z = state_of(a.seedA, kTruncateWords * ((kind == 2 ? a.tokens * c.heads * c.dim : 0) + at));
+        const uint64_t z = state_of(a.seedA, kTruncateWords * ((kind == 2 ? a.queries_at : 0) + at));
         truncate_numbers<N>(y0, a.frac, z);
         truncate_numbers<N>(y1, a.frac, z + (uint64_t)(kTruncateWords * apart) * kGamma);
     }
