@@ -347,7 +347,7 @@ HB_API int hb_cache_append(const hb_cache *cache, const int64_t *k0, const int64
  * workspace: DEVICE, 256-byte aligned, hb_attention_workspace_bytes(cache, batch, q_heads, max_len) bytes or more (0 for invalid sizes; of `cache` the
  * sizes count; no smaller batch or max_len needs more, so that one of the greatest serves every step), overlapping nothing; contents before and
  * after mean nothing; calls that may overlap in time need one each.  batch <= 65535, max_len <= HB_ATTENTION_MAX_LEN,
- * batch x q_heads x max_len <= HB_MAX_ELEMENTS.
+ * batch x q_heads x max_len <= HB_MAX_ELEMENTS.  Time grows with max_len too, not with the lengths alone: the ReLU goes over all places.
  * opened_bits receives 192 batch q_heads dim + n (128 + hb_opened_bits per element), n = batch q_heads max_len.
  */
 HB_API int hb_attention(const hb_cache *cache, const int64_t *q0, const int64_t *q1, size_t batch, int q_heads, const int32_t *page_table,

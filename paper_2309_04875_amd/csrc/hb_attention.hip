@@ -196,8 +196,8 @@ int hb_cache_append(const hb_cache *cache, const int64_t *k0, const int64_t *k1,
         a.rot = (uint32_t)rot;
         a.frac = frac;
         a.q_mul = q_mul;
-        // N = 2 from a workgroup for each compute unit on: below it a thread's time is the launch's (8 tokens of 48 heads of 128 4.5 us with N = 1, 5.0
-        // with 2; 333 of 36 heads of 80 9.5 and 8.8).
+        // N = 2 from a workgroup for each compute unit on: below it a thread's time is the launch's (8 tokens of 48 heads of 128 4.1 us with N = 1, 4.6
+        // with 2; 128 of them 8.4 and 7.8; 333 of 36 heads of 80 10.4 and 9.1).
         const uint64_t numbers = (uint64_t)tokens * (2 * (uint64_t)cache->heads + q_heads) * cache->dim;
         const int n = rot % 4 == 0 && cache->dim % 4 == 0 && numbers >= 4ull * 256 * hb::kAppendBlock ? 2 : 1, groups = cache->dim / (2 * n);      // of a head
         const uint64_t of_each = (uint64_t)cache->heads * groups, of_queries = (uint64_t)q_heads * groups, most = hb::append_launch_tokens(of_each, of_queries);

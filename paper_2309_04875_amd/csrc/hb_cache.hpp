@@ -85,7 +85,7 @@ __device__ __forceinline__ void open_numbers(const Pair (&y)[N], uint64_t z, uin
 // truncation, and every number of the cache two for its mask, 18 instructions each.  A thread takes N neighbours (dimensions d ..) and the N that
 // turn with them (d + rot/2 ..; the next N elsewhere), so that both multiply the same row of the tables and a number's words are drawn in step;
 // N = 2 (16-byte accesses, half the addresses) where the rotated part and the rest divide into such groups: 2048 tokens of 8 + 8 + 32 heads of 128,
-// 370 MB, in 76 us (4.9 TB/s) instead of 80.  Keys, values and queries have workgroups of their own, whose wavefronts then do the same.  The groups
+// 370 MB, in 73 us (5.1 TB/s) instead of 80.  Keys, values and queries have workgroups of their own, whose wavefronts then do the same.  The groups
 // of a token are shared out to workgroups, or several tokens with few share one.
 template <int N>
 __global__ void __launch_bounds__(kAppendBlock)

@@ -63,7 +63,7 @@ __device__ __forceinline__ void store_digits(uint8_t *planes, uint32_t lane, con
 
 // A step's weights of a tile, 16 rows of 128 bytes: lane l loads 16 bytes l mod 8 of rows l / 8 and l / 8 + 8, and they go through LDS to where the matrix
 // instruction takes them.  (Loaded from there at once, 16 rows by 64 bytes an instruction, 16 cache lines are asked for in each quarter of it:
-// 64 x (4096 -> 16384) 97 us for 109, 1 x (4096 -> 4096) 5.0 for 5.5, 64 x (4096 -> 16384) in groups of 32 169 for 339.)
+// 64 x (4096 -> 16384) 97 us for 109, 1 x (4096 -> 4096) 5.0 for 5.5, 64 x (4096 -> 16384) in groups of 32, then eight rows by eight tiles, 217 for 339.)
 struct StepWeights {
     u32x4_t w[2];
 };
@@ -124,9 +124,10 @@ __device__ __forceinline__ void unpack_weights(uint32_t w, int &even, int &odd)
 // A workgroup goes through the inputs in blocks of WK * P steps, whose digits its wavefronts make together and all of them read (with
 // WN = P = 1 each makes its own); wavefront (wn, wk) multiplies steps wk, wk + WK, .. of a block with its own RT tiles.
 //
-// What bounds it: one row, the launch and the chain of loads, digits, product, join and truncation (4096 -> 4096, 9 MB, 5.0 us); many rows, the scaling (five
-// instructions for two matrix instructions) and the digits, on the vector ALU, and the matrix instructions, which overlap little with them
-// (64 rows, 4096 -> 16384, 137 T operations, 93 us: VALU 37 % of the cycles, matrix cores 27 %).
+// What bounds it: one row, the launch and the chain of loads, digits, product, join and truncation (4096 -> 4096, 9 MB, 4.9 us); many rows, waiting: of the
+// 214,000 cycles of 64 rows, 4096 -> 16384, 137 G int8 operations, 93 us, the vector ALU takes 42 % (scaling, five instructions for two matrix instructions, and
+// digits), the matrix cores 31 %, and these overlap little; the rest are loads, LDS and barriers that two wavefronts a SIMD, all that their
+// registers leave, do not cover.
 template <int TM, int RT, int WN, int WK, int P, int FLUSH>
 __global__ void __launch_bounds__(64 * WN * WK, (TM * RT <= (FLUSH == 32 ? 4 : 8) && WN * WK == 8 ? 4 : 2))
 linear_q4_kernel(LinearArgs a)
