@@ -107,7 +107,7 @@ AttentionLayout attention_layout(const hb_cache *cache, size_t batch, int q_head
     lay.parts = 2 * scores;
     // Pieces of all sequences at most, also of fewer and shorter ones: as many as are cut together (512 / heads), or 1024 / heads and one more a sequence, or as
     // one sum's most places make; a unit each at least.
-    const size_t share = std::max<size_t>(units(1024, heads), 1), pieces = std::max(batch + share, batch * units(max_len, hb::kMostPlaces));
+    const size_t pieces = std::max(batch + units(1024, heads), batch * units(max_len, hb::kMostPlaces));
     lay.bytes = 2 * scores + round_up(16 * numbers * std::min(pieces, batch * units(max_len, hb::kValueUnit)));
     return lay;
 }

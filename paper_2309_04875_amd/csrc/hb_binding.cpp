@@ -387,13 +387,13 @@ bool take_cache(PyObject *const *a, hb_cache &c)
     return true;
 }
 
-// cache(keys, values, page_seeds) -> True: they are a cache's
+// cache(keys, values, page_seeds) -> the bytes of their struct hb_cache
 PyObject *cache(PyObject *, PyObject *const *a, Py_ssize_t count)
 {
     return guarded([&]() -> PyObject * {
         hb_cache c = {};
         if (count != 3 || !take_cache(a, c)) return not_known();
-        Py_RETURN_TRUE;
+        return PyBytes_FromStringAndSize(reinterpret_cast<const char *>(&c), sizeof(c));
     });
 }
 
@@ -492,7 +492,7 @@ PyMethodDef g_methods[] = {
     HB_FAST(eco_scan, "zero-error scan"),
     HB_FAST(party, "party-faithful ReLU"),
     HB_FAST(linear, "linear layer with 4-bit weights"),
-    HB_FAST(cache, "tensors of a paged cache"),
+    HB_FAST(cache, "struct of a paged cache"),
     HB_FAST(append, "keys and values into a paged cache"),
     HB_FAST(attention, "attention over a paged cache"),
     {"plan_run", plan_run, METH_O, "enqueue a plan"},

@@ -670,23 +670,26 @@ class Cache:
 
     def __init__(self, keys, values, page_seeds):
         self.keys, self.values, self.page_seeds = keys, values, page_seeds
-        if _native.cache(keys, values, page_seeds) is NotImplemented:
-            _cache_arg(self)
+        self.struct
 
     @property
     def struct(self):
-        return bytes(_cache_arg(self))
+        """The bytes of its struct, of the tensors as they are now."""
+        keys, values, page_seeds = self.keys, self.values, self.page_seeds
+        made = _native.cache(keys, values, page_seeds)
+        if made is NotImplemented:
+            import torch
+            at = _typed(keys, torch.int64, None, None, None, None), _typed(values, torch.int64, *keys.shape), _typed(page_seeds, torch.int64, keys.shape[0])
+            if max(keys.shape[1:]) >= 1 << 31:
+                raise ValueError("a cache's sizes are ints")
+            made = bytes(hb_cache(*at, *keys.shape))
+        return made
 
 
 def _cache_arg(cache):
-    import torch
     if not isinstance(cache, Cache):
         raise TypeError("expected a Cache")
-    keys, values, page_seeds = cache.keys, cache.values, cache.page_seeds
-    at = _typed(keys, torch.int64, None, None, None, None), _typed(values, torch.int64, *keys.shape), _typed(page_seeds, torch.int64, keys.shape[0])
-    if max(keys.shape[1:]) >= 1 << 31:
-        raise ValueError("a cache's sizes are ints")
-    return hb_cache(*at, *keys.shape)
+    return hb_cache.from_buffer_copy(cache.struct)
 
 
 def hb_cache_append(cache, k0, k1, v0, v1, slots, positions, cos, sin, frac, seed, q0=None, q1=None, q_mul=0, q_out0=None, q_out1=None,
